@@ -434,6 +434,83 @@ dnns_status dnns_deflate(const void* src_dev, size_t n_bytes, void* stream_dev, 
 dnns_status dnns_inflate(const void* stream_dev, size_t stream_bytes, const uint64_t* chunk_offset_dev,
                          const uint32_t* sub_bits_dev, size_t n_bytes, void* dst_dev, uint32_t* status_dev, void* stream);
 
+/*
+ * Variants in 8 bits.  A rebuilt variant of a language model runs with its weights and activations in 8 bits;
+ * these calls make them and compute with them.  They need no plan: plain device buffers, one format.
+ *
+ * "Rows in 8 bits": a matrix of rows x cols values is held as
+ *   q      int8 in [-127, 127], row r at q + r*ldq; q and ldq multiples of 16 (dnns_quantized_row_bytes(cols) is the
+ *          least ldq).  The bytes of a row past cols are never read and never written.
+ *   scale  fp32, one a row: q*scale stands for the value.
+ * Q(y) of a row y (fp32):  a = max |y|,  scale = a / 127,  q = y * (127 / a) rounded to nearest even.  A row of zeros
+ * gets scale 0 and q 0; a row with an Inf or a NaN gets scale NaN and q 0, so that whatever is computed from it is NaN
+ * too.  `values` (nullable) receives q*scale rounded to bf16, rows of ldv elements: what a fine-tuning step with the
+ * rounding in the loop goes on with (the rounding itself is passed straight through by the gradients below).
+ *
+ * Common rules
+ *   - Matrices of element type dtype (DNNS_F32 / DNNS_BF16) are row-major with unit column stride; ld* counts
+ *     elements from row to row and is at least the number of columns (rows may be pieces of wider ones).  Pointers need
+ *     the alignment of their element only; rows that start on 16 bytes are fastest.
+ *   - Arithmetic, sums and scales are fp32 (the product's sums are exact int32), rounded once where a result is stored.
+ *     No call uses atomics on floating point: the same inputs give the same bits.
+ *   - Outputs do not overlap inputs, except where a call says so.  rows == 0 does nothing (a gradient that is a sum over
+ *     rows is then zero); cols == 0 gives scale 0 for every row.
+ *   - Errors: INVALID_ARG (null or misaligned pointer, negative size, an ld below its columns, eps), UNSUPPORTED
+ *     (dtype; more than 2^31 - 1 rows or columns; a matrix of 2^62 bytes or more), CUDA.
+ */
+size_t dnns_quantized_row_bytes(size_t cols); /* cols rounded up to a multiple of 16 */
+
+/* Q of every row of x: weights per output channel (x a rebuilt [O][I] tensor, which dnns_compact left in an arena with
+ * ldx = I), or the tokens of an activation. */
+dnns_status dnns_quantize_rows(const void* x, int64_t ldx, int32_t dtype, int64_t rows, int64_t cols, int8_t* q, int64_t ldq,
+                               float* scale, uint16_t* values, int64_t ldv, void* stream);
+
+/*
+ * Root-mean-square norm with the residual's addition, in 8 bits:
+ *   h = x + residual (residual nullable: h = x),   y = h * weight / sqrt(mean(h^2) + eps)  (weight fp32, nullable: 1)
+ *   q, scale, values = Q(y);   h_out (nullable, dtype) = h.
+ * h_out may be x or residual itself (same pointer and ld): the residual stream updated in place.  eps is at least 2^-126.
+ * A row whose sum of squares is not finite in fp32 counts as one with an Inf.
+ */
+dnns_status dnns_rmsnorm_quantize(const void* x, int64_t ldx, const void* residual, int64_t ldr, const float* weight, float eps,
+                            int32_t dtype, int64_t rows, int64_t cols, void* h_out, int64_t ldh, int8_t* q, int64_t ldq,
+                            float* scale, uint16_t* values, int64_t ldv, void* stream);
+/*
+ * Its gradient at h, rounding passed straight through.  With r = 1 / sqrt(mean(h^2) + eps) and g = dy * weight:
+ *   dx = r * (g - h*r * mean(g * h*r)) + dh   (dh nullable: the gradient that reaches h past the norm),
+ * which is the gradient of x and of residual alike, and dweight (fp32 [cols], nullable) = sum over rows of dy * h * r.
+ * dx may be dy, h or dh itself.  ws_dev (16-byte aligned, dnns_rmsnorm_backward_workspace_bytes; only for dweight)
+ * receives the partial sums of row groups, which a second kernel adds in a fixed order.  Errors: also WORKSPACE.
+ */
+size_t dnns_rmsnorm_backward_workspace_bytes(int64_t rows, int64_t cols);
+dnns_status dnns_rmsnorm_backward(const void* dy, int64_t lddy, const void* h, int64_t ldh, const float* weight, float eps,
+                                     const void* dh, int64_t lddh, int32_t dtype, int64_t rows, int64_t cols, void* dx,
+                                     int64_t lddx, float* dweight, void* ws_dev, size_t ws_bytes, void* stream);
+
+/*
+ * The gated activation between the products of a block, in 8 bits:  Q(silu(gate) * up),  silu(g) = g / (1 + exp(-g)).
+ * gate and up are often the halves of one product's rows.  The gradient (rounding passed straight through), with
+ * s = 1 / (1 + exp(-gate)):  dgate = dy * up * s * (1 + gate * (1 - s)),  dup = dy * gate * s.
+ * dgate and dup may be dy, gate or up themselves (same pointer and ld).
+ */
+dnns_status dnns_silu_gate_quantize(const void* gate, int64_t ldg, const void* up, int64_t ldu, int32_t dtype, int64_t rows,
+                              int64_t cols, int8_t* q, int64_t ldq, float* scale, uint16_t* values, int64_t ldv, void* stream);
+dnns_status dnns_silu_gate_backward(const void* dy, int64_t lddy, const void* gate, int64_t ldg, const void* up, int64_t ldu,
+                                       int32_t dtype, int64_t rows, int64_t cols, void* dgate, int64_t lddg, void* dup,
+                                       int64_t lddu, void* stream);
+
+/*
+ * Product of rows in 8 bits:  y[t][n] = (sum_k xq[t][k] * wq[n][k]) * xscale[t] * wscale[n] + bias[n]
+ * for rows tokens, in_cols columns and out_cols output channels; y has element type dtype, rows of ldy elements; bias
+ * (fp32, nullable).  The sum is exact: in_cols is at most DNNS_LINEAR_MAX_IN (UNSUPPORTED above), so that int32 holds it.
+ * in_cols == 0 leaves the bias.  Every wait of the kernels is bounded; one that runs out ends the kernel, leaves y
+ * incomplete and sets *status_dev (device word, cleared by the caller) to DNNS_ERR_TIMEOUT.
+ */
+#define DNNS_LINEAR_MAX_IN 131071
+dnns_status dnns_linear_quantized(const int8_t* xq, int64_t ldx, const float* xscale, const int8_t* wq, int64_t ldw, const float* wscale,
+                           const float* bias, int64_t rows, int64_t in_cols, int64_t out_cols, int32_t dtype, void* y,
+                           int64_t ldy, uint32_t* status_dev, void* stream);
+
 /* Synchronises `stream`, then returns (and clears) the status recorded by the plan's kernels. */
 dnns_status dnns_last_device_status(dnns_plan* plan, void* stream);
 

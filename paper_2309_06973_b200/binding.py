@@ -21,11 +21,14 @@ DNNS_STATIC_MAX_NUMEL = 1 << 26
 DNNS_DEFLATE_CHUNK, DNNS_DEFLATE_SUB = 16384, 512
 DNNS_MULTI_MAX = 4
 DNNS_PORTFOLIO_MAX = 16
+DNNS_LINEAR_MAX_IN = 131071
 
 EXPORTS = ["dnns_status_string", "dnns_workspace_bytes", "dnns_plan_create", "dnns_plan_destroy", "dnns_plan_layout",
            "dnns_plan_launch_count", "dnns_magnitude_threshold", "dnns_apply_mask", "dnns_zero_structures",
            "dnns_propagate_keep", "dnns_compact", "dnns_last_device_status", "dnns_magnitude_threshold_static", "dnns_mask_and_structures", "dnns_fold_batchnorm", "dnns_propagate_keep_cascade",
-           "dnns_plan_profile", "dnns_plan_profile_read", "dnns_plan_tie_sweep", "dnns_mask_and_structures_multi", "dnns_propagate_keep_multi", "dnns_compact_masked", "dnns_zero_structures_portfolio", "dnns_compact_masked_multi", "dnns_deflate_chunks", "dnns_deflate_bound", "dnns_deflate_workspace_bytes", "dnns_deflate", "dnns_inflate"]
+           "dnns_plan_profile", "dnns_plan_profile_read", "dnns_plan_tie_sweep", "dnns_mask_and_structures_multi", "dnns_propagate_keep_multi", "dnns_compact_masked", "dnns_zero_structures_portfolio", "dnns_compact_masked_multi", "dnns_deflate_chunks", "dnns_deflate_bound", "dnns_deflate_workspace_bytes", "dnns_deflate", "dnns_inflate",
+           "dnns_quantized_row_bytes", "dnns_quantize_rows", "dnns_rmsnorm_quantize", "dnns_rmsnorm_backward_workspace_bytes",
+           "dnns_rmsnorm_backward", "dnns_silu_gate_quantize", "dnns_silu_gate_backward", "dnns_linear_quantized"]
 
 
 class dnns_tensor(C.Structure):
@@ -117,6 +120,17 @@ def lib() -> C.CDLL:
             getattr(L, name).argtypes = [C.c_size_t]
         L.dnns_deflate.argtypes = [vp, C.c_size_t, vp, C.c_size_t, vp, vp, vp, C.c_size_t, vp]
         L.dnns_inflate.argtypes = [vp, C.c_size_t, vp, vp, C.c_size_t, vp, vp, vp]
+        i64, f32 = C.c_int64, C.c_float
+        L.dnns_quantized_row_bytes.restype = C.c_size_t
+        L.dnns_quantized_row_bytes.argtypes = [C.c_size_t]
+        L.dnns_quantize_rows.argtypes = [vp, i64, i32, i64, i64, vp, i64, vp, vp, i64, vp]
+        L.dnns_rmsnorm_quantize.argtypes = [vp, i64, vp, i64, vp, f32, i32, i64, i64, vp, i64, vp, i64, vp, vp, i64, vp]
+        L.dnns_rmsnorm_backward_workspace_bytes.restype = C.c_size_t
+        L.dnns_rmsnorm_backward_workspace_bytes.argtypes = [i64, i64]
+        L.dnns_rmsnorm_backward.argtypes = [vp, i64, vp, i64, vp, f32, vp, i64, i32, i64, i64, vp, i64, vp, vp, C.c_size_t, vp]
+        L.dnns_silu_gate_quantize.argtypes = [vp, i64, vp, i64, i32, i64, i64, vp, i64, vp, vp, i64, vp]
+        L.dnns_silu_gate_backward.argtypes = [vp, i64, vp, i64, vp, i64, i32, i64, i64, vp, i64, vp, i64, vp]
+        L.dnns_linear_quantized.argtypes = [vp, i64, vp, vp, i64, vp, vp, i64, i64, i64, i32, vp, i64, vp, vp]
         _lib = L
     return _lib
 
@@ -296,3 +310,49 @@ def dnns_compact_masked(plan, thr_dev: int, variant: int, keep_idx: int, keep_co
                         dst_bytes: int, dst_offsets_dev: int, dst_shapes_dev: int, stream: int = 0) -> None:
     _check(lib().dnns_compact_masked(plan, thr_dev, variant, keep_idx, keep_count, dst_arena, dst_bytes,
                                      dst_offsets_dev, dst_shapes_dev, stream), "dnns_compact_masked")
+
+
+# ---- variants in 8 bits (device addresses; 0 or None where a pointer is nullable) ----
+def dnns_quantized_row_bytes(cols: int) -> int:
+    return lib().dnns_quantized_row_bytes(cols)
+
+
+def dnns_quantize_rows(x: int, ldx: int, dtype: int, rows: int, cols: int, q: int, ldq: int, scale: int, values: int = 0,
+                       ldv: int = 0, stream: int = 0) -> None:
+    _check(lib().dnns_quantize_rows(x, ldx, dtype, rows, cols, q, ldq, scale, values or None, ldv, stream), "dnns_quantize_rows")
+
+
+def dnns_rmsnorm_quantize(x: int, ldx: int, residual: int, ldr: int, weight: int, eps: float, dtype: int, rows: int, cols: int,
+                          h_out: int, ldh: int, q: int, ldq: int, scale: int, values: int = 0, ldv: int = 0,
+                          stream: int = 0) -> None:
+    _check(lib().dnns_rmsnorm_quantize(x, ldx, residual or None, ldr, weight or None, eps, dtype, rows, cols, h_out or None, ldh,
+                                       q, ldq, scale, values or None, ldv, stream), "dnns_rmsnorm_quantize")
+
+
+def dnns_rmsnorm_backward_workspace_bytes(rows: int, cols: int) -> int:
+    return lib().dnns_rmsnorm_backward_workspace_bytes(rows, cols)
+
+
+def dnns_rmsnorm_backward(dy: int, lddy: int, h: int, ldh: int, weight: int, eps: float, dh: int, lddh: int, dtype: int,
+                          rows: int, cols: int, dx: int, lddx: int, dweight: int, ws_dev: int, ws_bytes: int,
+                          stream: int = 0) -> None:
+    _check(lib().dnns_rmsnorm_backward(dy, lddy, h, ldh, weight or None, eps, dh or None, lddh, dtype, rows, cols, dx, lddx,
+                                       dweight or None, ws_dev or None, ws_bytes, stream), "dnns_rmsnorm_backward")
+
+
+def dnns_silu_gate_quantize(gate: int, ldg: int, up: int, ldu: int, dtype: int, rows: int, cols: int, q: int, ldq: int,
+                            scale: int, values: int = 0, ldv: int = 0, stream: int = 0) -> None:
+    _check(lib().dnns_silu_gate_quantize(gate, ldg, up, ldu, dtype, rows, cols, q, ldq, scale, values or None, ldv, stream),
+           "dnns_silu_gate_quantize")
+
+
+def dnns_silu_gate_backward(dy: int, lddy: int, gate: int, ldg: int, up: int, ldu: int, dtype: int, rows: int, cols: int,
+                            dgate: int, lddg: int, dup: int, lddu: int, stream: int = 0) -> None:
+    _check(lib().dnns_silu_gate_backward(dy, lddy, gate, ldg, up, ldu, dtype, rows, cols, dgate, lddg, dup, lddu, stream),
+           "dnns_silu_gate_backward")
+
+
+def dnns_linear_quantized(xq: int, ldx: int, xscale: int, wq: int, ldw: int, wscale: int, bias: int, rows: int, in_cols: int,
+                          out_cols: int, dtype: int, y: int, ldy: int, status_dev: int, stream: int = 0) -> None:
+    _check(lib().dnns_linear_quantized(xq or None, ldx, xscale, wq or None, ldw, wscale, bias or None, rows, in_cols, out_cols,
+                                       dtype, y, ldy, status_dev, stream), "dnns_linear_quantized")

@@ -388,3 +388,141 @@ class Deflater:
         nc = B.dnns_deflate_chunks(self.n_bytes)
         return (self.chunk_offset[: nc + 1].cpu().numpy().view(np.uint64).copy(),
                 self.sub_bits[: 32 * nc].cpu().numpy().view(np.uint32).copy())
+
+
+# ---- variants in 8 bits ------------------------------------------------------------------------------------
+_DTYPE = {torch.float32: B.DNNS_F32, torch.bfloat16: B.DNNS_BF16}
+
+
+def _matrix(t: torch.Tensor, rows: int, cols: int, dtype, what: str):
+    """(address, row stride) of a rows x cols device matrix with unit column stride; raises on anything else."""
+    if t.dtype is not dtype or not t.is_cuda or t.shape != (rows, cols) or (cols > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: a {rows} x {cols} {dtype} CUDA matrix with unit column stride is needed, "
+                         f"got {tuple(t.shape)} {t.dtype} strides {t.stride()} on {t.device}")
+    return t.data_ptr(), t.stride(0) if rows > 1 else max(cols, t.stride(0))
+
+
+def _vector(t: torch.Tensor, n: int, what: str) -> int:
+    if t.dtype is not torch.float32 or not t.is_cuda or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous float32 CUDA vector of {n} is needed, got {tuple(t.shape)} {t.dtype}")
+    return t.data_ptr()
+
+
+def _dtype_of(t: torch.Tensor, what: str) -> int:
+    d = _DTYPE.get(t.dtype)
+    if d is None or t.dim() != 2:
+        raise ValueError(f"{what}: a float32 or bfloat16 matrix is needed, got {t.dim()} dimensions of {t.dtype}")
+    return d
+
+
+class RowsQ8:
+    """A matrix held as rows in 8 bits: ``q`` (int8, rows padded to start on 16 bytes), ``scale`` (float32, one a row)
+    and, on request, ``values`` (bfloat16: q * scale)."""
+
+    def __init__(self, rows: int, cols: int, device="cuda:0", values: bool = False):
+        self._set(torch.empty(rows, B.dnns_quantized_row_bytes(cols), dtype=torch.int8, device=device),
+                  torch.empty(rows, dtype=torch.float32, device=device), cols,
+                  torch.empty(rows, cols, dtype=torch.bfloat16, device=device) if values else None)
+
+    @classmethod
+    def of(cls, q: torch.Tensor, scale: torch.Tensor, cols: int, values: Optional[torch.Tensor] = None) -> "RowsQ8":
+        """Rows that exist already: q (rows, at least cols) of int8, its rows 16-byte aligned."""
+        self = cls.__new__(cls)
+        self._set(q, scale, cols, values)
+        return self
+
+    def _set(self, q, scale, cols, values):
+        if q.dtype is not torch.int8 or q.dim() != 2 or not q.is_cuda or q.shape[1] < cols or (q.shape[1] > 1 and q.stride(1) != 1):
+            raise ValueError(f"q: an int8 CUDA matrix of at least {cols} columns is needed, got {tuple(q.shape)} {q.dtype}")
+        self.rows, self.cols, self.q, self.scale, self.values = q.shape[0], cols, q, scale, values
+        self.device = q.device
+        self.q_ptr, self.ld = q.data_ptr(), q.stride(0) if self.rows > 1 else B.dnns_quantized_row_bytes(cols)
+        self.scale_ptr = _vector(scale, self.rows, "scale")
+        self.values_ptr, self.ldv = (0, 0) if values is None else _matrix(values, self.rows, cols, torch.bfloat16, "values")
+
+
+def quantize_rows(x: torch.Tensor, out: RowsQ8) -> RowsQ8:
+    """The rows of x in 8 bits: a weight matrix per output channel, or an activation per token."""
+    dtype = _dtype_of(x, "x")
+    p, ld = _matrix(x, out.rows, out.cols, x.dtype, "x")
+    B.dnns_quantize_rows(p, ld, dtype, out.rows, out.cols, out.q_ptr, out.ld, out.scale_ptr, out.values_ptr, out.ldv, _stream())
+    return out
+
+
+def rmsnorm_q8(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float, out: RowsQ8,
+               residual: Optional[torch.Tensor] = None, h: Optional[torch.Tensor] = None) -> RowsQ8:
+    """h = x + residual (stored when given; may be x or residual), out = h * weight / sqrt(mean(h^2) + eps) in 8 bits."""
+    dtype, rows, cols = _dtype_of(x, "x"), out.rows, out.cols
+    p, ld = _matrix(x, rows, cols, x.dtype, "x")
+    pr, ldr = (0, 0) if residual is None else _matrix(residual, rows, cols, x.dtype, "residual")
+    ph, ldh = (0, 0) if h is None else _matrix(h, rows, cols, x.dtype, "h")
+    B.dnns_rmsnorm_quantize(p, ld, pr, ldr, 0 if weight is None else _vector(weight, cols, "weight"), eps, dtype, rows, cols, ph, ldh,
+                            out.q_ptr, out.ld, out.scale_ptr, out.values_ptr, out.ldv, _stream())
+    return out
+
+
+def rmsnorm_q8_backward_workspace(rows: int, cols: int, device="cuda:0") -> torch.Tensor:
+    return torch.empty(max(16, B.dnns_rmsnorm_backward_workspace_bytes(rows, cols)), dtype=torch.uint8, device=device)
+
+
+def rmsnorm_q8_backward(dy: torch.Tensor, h: torch.Tensor, weight: Optional[torch.Tensor], eps: float, dx: torch.Tensor,
+                        dweight: Optional[torch.Tensor] = None, dh: Optional[torch.Tensor] = None,
+                        workspace: Optional[torch.Tensor] = None) -> None:
+    """The norm's gradient at h: dx (of x and residual alike; dh, the gradient that reaches h past the norm, added) and
+    dweight, which needs a workspace."""
+    dtype, (rows, cols) = _dtype_of(h, "h"), h.shape
+    m = lambda t, what: (0, 0) if t is None else _matrix(t, rows, cols, h.dtype, what)
+    pdy, lddy = m(dy, "dy")
+    ph, ldh = m(h, "h")
+    pdh, lddh = m(dh, "dh")
+    pdx, lddx = m(dx, "dx")
+    B.dnns_rmsnorm_backward(pdy, lddy, ph, ldh, 0 if weight is None else _vector(weight, cols, "weight"), eps, pdh, lddh, dtype,
+                            rows, cols, pdx, lddx, 0 if dweight is None else _vector(dweight, cols, "dweight"),
+                            0 if workspace is None else workspace.data_ptr(),
+                            0 if workspace is None else workspace.numel() * workspace.element_size(), _stream())
+
+
+def silu_gate_q8(gate: torch.Tensor, up: torch.Tensor, out: RowsQ8) -> RowsQ8:
+    """out = silu(gate) * up in 8 bits."""
+    dtype = _dtype_of(gate, "gate")
+    pg, ldg = _matrix(gate, out.rows, out.cols, gate.dtype, "gate")
+    pu, ldu = _matrix(up, out.rows, out.cols, gate.dtype, "up")
+    B.dnns_silu_gate_quantize(pg, ldg, pu, ldu, dtype, out.rows, out.cols, out.q_ptr, out.ld, out.scale_ptr, out.values_ptr,
+                              out.ldv, _stream())
+    return out
+
+
+def silu_gate_q8_backward(dy: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, dgate: torch.Tensor, dup: torch.Tensor) -> None:
+    """Gradients of gate and up."""
+    dtype, (rows, cols) = _dtype_of(gate, "gate"), gate.shape
+    a = []
+    for t, what in ((dy, "dy"), (gate, "gate"), (up, "up"), (dgate, "dgate"), (dup, "dup")):
+        a.append(_matrix(t, rows, cols, gate.dtype, what))
+    B.dnns_silu_gate_backward(*a[0], *a[1], *a[2], dtype, rows, cols, *a[3], *a[4], _stream())
+
+
+class LinearQ8:
+    """A layer whose weights are rows in 8 bits (a scale per output channel), applied to tokens in 8 bits."""
+
+    def __init__(self, weight: RowsQ8, bias: Optional[torch.Tensor] = None):
+        self.weight, self.bias = weight, bias
+        self.bias_ptr = 0 if bias is None else _vector(bias, weight.rows, "bias")
+        self.status = torch.zeros(1, dtype=torch.int32, device=weight.device)
+        self._status_ptr = self.status.data_ptr()
+
+    def __call__(self, x: RowsQ8, y: torch.Tensor) -> torch.Tensor:
+        """y (x.rows, weight.rows) of float32 or bfloat16 = x . weight^T + bias."""
+        w = self.weight
+        if x.cols != w.cols:
+            raise ValueError(f"x has {x.cols} columns, the layer {w.cols}")
+        dtype = _dtype_of(y, "y")
+        p, ld = _matrix(y, x.rows, w.rows, y.dtype, "y")
+        B.dnns_linear_quantized(x.q_ptr, x.ld, x.scale_ptr, w.q_ptr, w.ld, w.scale_ptr, self.bias_ptr, x.rows, x.cols, w.rows,
+                                dtype, p, ld, self._status_ptr, _stream())
+        return y
+
+    def device_status(self) -> int:
+        """Synchronises and returns (and clears) the status the layer's kernels recorded."""
+        s = int(self.status.item())
+        self.status.zero_()
+        return s
