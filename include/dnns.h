@@ -456,7 +456,7 @@ dnns_status dnns_inflate(const void* stream_dev, size_t stream_bytes, const uint
  *   - Outputs do not overlap inputs, except where a call says so.  rows == 0 does nothing (a gradient that is a sum over
  *     rows is then zero); cols == 0 gives scale 0 for every row.
  *   - Errors: INVALID_ARG (null or misaligned pointer, negative size, an ld below its columns, eps), UNSUPPORTED
- *     (dtype; more than 2^31 - 1 rows or columns; a matrix of 2^62 bytes or more), CUDA.
+ *     (dtype; more than 2^31 - 1 rows, or columns: 2^30 in a matrix of values; a matrix of 2^62 bytes or more), CUDA.
  */
 size_t dnns_quantized_row_bytes(size_t cols); /* cols rounded up to a multiple of 16 */
 

@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "dnns.h"
 
 namespace dnns {
@@ -318,6 +320,15 @@ struct FoldJob {
 int launch_fold(const Tables& tb, void* arena, const uint64_t* offsets, const int32_t* shapes, uint32_t* job_count,
                 FoldJob* jobs, int n_sm, cudaStream_t st);
 cudaError_t init_kernel_attributes();
+// Lets a kernel use `bytes` of dynamic shared memory, once per device (`done`: a static word of the caller, a bit per device).
+template <typename F>
+inline bool allow_shared(F* kernel, size_t bytes, std::atomic<uint64_t>& done, int dev) {
+    const uint64_t bit = 1ull << (dev & 63);
+    if (dev < 64 && (done.load(std::memory_order_relaxed) & bit)) return true;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return false;
+    if (dev < 64) done.fetch_or(bit, std::memory_order_relaxed);
+    return true;
+}
 cudaError_t init_compact_attributes();
 constexpr uint32_t kGatherStageBytes = 18432;  // one stage buffer of the staged rebuild
 constexpr uint32_t kGatherPieceBytes = 2304;   // longest piece of a row in a unit (64 channels of a 3x3 fp32 filter)

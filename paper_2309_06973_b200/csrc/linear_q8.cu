@@ -14,7 +14,6 @@
 #include <cuda.h>
 
 #include <algorithm>
-#include <atomic>
 
 #include "dnns_internal.cuh"
 
@@ -569,16 +568,6 @@ bool make_map(CUtensorMap* map, const int8_t* p, int64_t rows, int64_t k, int64_
     const cuuint32_t box[2] = {kBlockK, box_rows}, steps[2] = {1, 1};
     return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t*>(p), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-// Lets a kernel use its shared memory, once per device.
-template <typename F>
-bool allow_shared(F* kernel, uint32_t bytes, std::atomic<uint64_t>& done, int dev) {
-    const uint64_t bit = 1ull << (dev & 63);
-    if (dev < 64 && (done.load(std::memory_order_relaxed) & bit)) return true;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return false;
-    if (dev < 64) done.fetch_or(bit, std::memory_order_relaxed);
-    return true;
 }
 
 template <int BT, int DT>

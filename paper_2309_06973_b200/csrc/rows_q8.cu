@@ -2,16 +2,19 @@
 // root-mean-square norm with the residual's addition, and the gated activation - and the gradients of those two.
 //   Q(y): a = max |y|, scale = a / 127, q = rint(y * 127 / a).
 //
-// All five are bound by memory: a few operations an element against 5 to 9 bytes of traffic.  So each row is read
+// All five are bound by memory: a few operations an element against 5 to 11 bytes of traffic.  So each row is read
 // once and kept in registers (fp32) between the reduction that its scale needs and the stores.  For the norm the
 // reduction is a single one, because q does not depend on the row's root mean square: with v = h * weight and
 // r = 1 / sqrt(mean(h^2) + eps), q = rint(v * 127 / max|v|) and scale = r * max|v| / 127, so the sum of squares and the
 // maximum travel through the same shuffles and the same barrier.
 //
-// A thread works on pieces of 8 columns.  Where every row of every matrix starts on 16 bytes (VEC) a piece is 8
-// neighbouring columns moved as 16-byte vectors; otherwise neighbouring threads take neighbouring columns, one element an
-// access, so that a warp still touches whole sectors.  NV pieces a thread: a row of up to 8 * NV * threads columns stays in
-// registers; longer rows (NV = 0) are walked twice.
+// A team of warps has a row (one warp for short rows, several teams a block).  A lane works on pieces of 8 neighbouring
+// columns; NV pieces a lane, so a row of up to 8 * NV * lanes columns stays in registers, and longer ones (NV = 0) are walked
+// twice.  Rows of a rebuilt layer have any width, so they start anywhere: SHIFT handles rows that do not start on 16 bytes
+// with the same 16-byte accesses.  A lane then fetches the two aligned vectors around its piece and shifts its 8 columns
+// out of them; it stores the aligned vector that ends inside its piece, whose front columns come from the lane before it
+// by shuffles.  The first lane of a warp repeats the piece of the previous warp's last lane, so that every stored vector finds its
+// front: 31 pieces a warp instead of 32.  Only the ends of a row go element by element.
 #include <algorithm>
 
 #include "dnns_internal.cuh"
@@ -22,9 +25,11 @@ namespace {
 
 constexpr uint32_t kFullMask = 0xFFFFFFFFu;
 constexpr uint32_t kInfBits = 0x7F800000u;
-constexpr int kMaxRowThreads = 1024;
-constexpr int kWarpRows = 8;       // rows per block where a warp has a row to itself
-constexpr int kBackThreads = 512;  // threads a row of the norm's gradient at most
+constexpr uint32_t kNanBits = 0x7FC00000u;
+constexpr int kBlockWarps = 8;  // warps of a block whose teams are small
+// Warps of a team at most, by pieces a lane: what keeps a row in registers without spilling.
+constexpr int quantize_warps(int nv) { return nv == 4 ? 16 : 32; }
+constexpr int backward_warps(int nv) { return nv == 2 ? 20 : 16; }
 
 template <int DT>
 struct Store;
@@ -48,97 +53,190 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
 __device__ __forceinline__ void narrow(float x, float& d) { d = x; }
 __device__ __forceinline__ void narrow(float x, uint16_t& d) { d = (uint16_t)bf16_pair(x, 0.0f); }
 
-// Column of element e of piece j of thread t.
-template <bool VEC>
-__device__ __forceinline__ int64_t column(int64_t j, int e, int t, int threads) {
-    return VEC ? (j * threads + t) * 8 + e : (j * 8 + e) * threads + t;
+// ---- pieces of 8 columns -------------------------------------------------------------------------------------
+// Where a lane's pieces are: team of `warps`, this one being number `warp`.
+template <bool SHIFT>
+struct Lanes {
+    static constexpr int kPieces = SHIFT ? 31 : 32;  // of a warp
+    int warps, warp, lane;
+    __device__ __forceinline__ int column(int j) const { return 8 * ((j * warps + warp) * kPieces + lane - (SHIFT ? 1 : 0)); }
+    // (SHIFT: lane 0's piece is the previous warp's; its values are counted there)
+    __device__ __forceinline__ bool counted() const { return !SHIFT || lane != 0; }
+};
+// pieces of a row; SHIFT: one more, since the columns at the end may be stored by the lane after the last piece
+template <bool SHIFT>
+__host__ __device__ inline int row_pieces(int cols) { return (cols + 7) / 8 + (SHIFT ? 1 : 0); }
+
+// Elements by which a row starts past a 16-byte boundary.
+template <typename T>
+__device__ __forceinline__ int row_shift(const T* row) { return (int)((reinterpret_cast<uintptr_t>(row) / sizeof(T)) & (16 / sizeof(T) - 1)); }
+
+// Words s .. of a run of words: s in 16-bit steps below 8 (bf16), in words below 4 (fp32).
+__device__ __forceinline__ void shift_out(const uint32_t (&w)[8], int s, uint32_t (&r)[4]) {
+    uint32_t t[6], u[5];
+#pragma unroll
+    for (int i = 0; i < 6; ++i) t[i] = s & 4 ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) u[i] = s & 2 ? t[i + 1] : t[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = __funnelshift_r(u[i], u[i + 1], 16 * (s & 1));
+}
+__device__ __forceinline__ void shift_out(const uint32_t (&w)[12], int s, uint32_t (&r)[8]) {
+    uint32_t t[9];
+#pragma unroll
+    for (int i = 0; i < 9; ++i) t[i] = s & 2 ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = s & 1 ? t[i + 1] : t[i];
+}
+__device__ __forceinline__ void widen8(const uint32_t (&w)[4], float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+}
+__device__ __forceinline__ void widen8(const uint32_t (&w)[8], float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
 }
 
-// Piece j of a row; columns past the end read as 0.
-template <bool VEC, typename T>
-__device__ __forceinline__ void load8(const T* row, int64_t j, int t, int threads, int64_t cols, float (&v)[8]) {
-    const int64_t c0 = column<VEC>(j, 0, t, threads);
-    if (VEC && c0 + 8 <= cols) {
-        if constexpr (sizeof(T) == 4) {
-            const float4 a = *reinterpret_cast<const float4*>(row + c0), b = *reinterpret_cast<const float4*>(row + c0 + 4);
-            v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-        } else {
-            const uint4 a = *reinterpret_cast<const uint4*>(row + c0);
-            const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+// Columns c .. c + 7 of a row; those outside it read as 0.  In two steps, so that all of a lane's loads are on their way
+// before the first of them is waited for: `fetch` issues the vector loads, predicated and without a branch, `get` shifts and
+// widens what came, and reads element by element where a vector would have left the row.
+template <bool SHIFT, typename T>
+struct Piece {
+    static constexpr int kPer = 16 / sizeof(T), kWords = 2 * sizeof(T);  // elements of a vector, words of a piece
+    uint32_t w[kWords + (SHIFT ? 4 : 0)];
+    static __device__ __forceinline__ bool whole(int c, int cols, int s) { return c >= s && c + 8 + (SHIFT && s ? kPer - s : 0) <= cols; }
+    __device__ __forceinline__ void fetch(const T* row, int c, int cols) {
+        const int s = SHIFT ? row_shift(row) : 0;
+        const bool in = whole(c, cols, s);
+        const T* p = row + (c - s);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+        for (int i = 0; i < kWords / 4 + (SHIFT ? 1 : 0); ++i) {
+            const bool need = in && (i < kWords / 4 || s);
+            w[4 * i] = w[4 * i + 1] = w[4 * i + 2] = w[4 * i + 3] = 0;
+            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %5, 0;\n\t@p ld.global.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+                         : "+r"(w[4 * i]), "+r"(w[4 * i + 1]), "+r"(w[4 * i + 2]), "+r"(w[4 * i + 3])
+                         : "l"(p + i * kPer), "r"((uint32_t)need)
+                         : "memory");
+        }
+    }
+    __device__ __forceinline__ void get(const T* row, int c, int cols, float (&v)[8]) const {
+        const int s = SHIFT ? row_shift(row) : 0;
+        if constexpr (SHIFT) {
+            uint32_t r[kWords];
+            shift_out(w, s, r);
+            widen8(r, v);
+        } else {
+            widen8(w, v);
+        }
+        if (!whole(c, cols, s) && c + 8 > 0 && c < cols) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (c + e >= 0 && c + e < cols) v[e] = widen(row[c + e]);
+        }
+    }
+};
+template <bool SHIFT, typename T>
+__device__ __forceinline__ void load8(const T* row, int c, int cols, float (&v)[8]) {
+    Piece<SHIFT, T> p;
+    p.fetch(row, c, cols);
+    p.get(row, c, cols, v);
+}
+
+// Stores columns c .. c + 7.  All lanes of the warp take part (SHIFT: a lane may store columns of the lane before it).
+template <bool SHIFT, typename T>
+__device__ __forceinline__ void store8(T* row, int c, int cols, const float (&v)[8]) {
+    constexpr int kPer = 16 / sizeof(T), kWords = 2 * sizeof(T);
+    uint32_t w[kWords + 4];  // behind the 4 words (SHIFT) of the lane before
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[4 + i] = __float_as_uint(v[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[4 + i] = bf16_pair(v[2 * i], v[2 * i + 1]);
+    }
+    const int s = SHIFT ? row_shift(row) : 0;
+    if (s == 0) {
+        if (SHIFT && (threadIdx.x & 31) == 0) return;  // the previous warp's
+        if (c >= 0 && c + 8 <= cols) {
+#pragma unroll
+            for (int i = 0; i < kWords / 4; ++i) *reinterpret_cast<uint4*>(row + c + i * kPer) = make_uint4(w[4 + 4 * i], w[5 + 4 * i], w[6 + 4 * i], w[7 + 4 * i]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (c + e >= 0 && c + e < cols) narrow(v[e], row[c + e]);
         }
         return;
     }
+    if constexpr (SHIFT) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int64_t c = column<VEC>(j, e, t, threads);
-        v[e] = c < cols ? widen(row[c]) : 0.0f;
-    }
-}
-
-template <bool VEC, typename T>
-__device__ __forceinline__ void store8(T* row, int64_t j, int t, int threads, int64_t cols, const float (&v)[8]) {
-    const int64_t c0 = column<VEC>(j, 0, t, threads);
-    if (VEC && c0 + 8 <= cols) {
-        if constexpr (sizeof(T) == 4) {
-            *reinterpret_cast<float4*>(row + c0) = make_float4(v[0], v[1], v[2], v[3]);
-            *reinterpret_cast<float4*>(row + c0 + 4) = make_float4(v[4], v[5], v[6], v[7]);
+        for (int i = 0; i < 4; ++i) w[i] = __shfl_up_sync(kFullMask, w[kWords + i], 1);
+        if ((threadIdx.x & 31) == 0) return;
+        uint32_t r[kWords];
+        shift_out(w, kPer - s, r);  // columns c - s ..
+        c -= s;
+        if (c >= 0 && c + 8 <= cols) {
+#pragma unroll
+            for (int i = 0; i < kWords / 4; ++i) *reinterpret_cast<uint4*>(row + c + i * kPer) = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
         } else {
-            *reinterpret_cast<uint4*>(row + c0) = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (c + e >= 0 && c + e < cols) {
+                    if constexpr (sizeof(T) == 4) row[c + e] = __uint_as_float(r[e]);
+                    else row[c + e] = (uint16_t)(r[e / 2] >> (16 * (e & 1)));
+                }
         }
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int64_t c = column<VEC>(j, e, t, threads);
-        if (c < cols) narrow(v[e], row[c]);
     }
 }
 
-template <bool VEC>
-__device__ __forceinline__ void store8_int(int8_t* row, int64_t j, int t, int threads, int64_t cols, const int (&q)[8]) {
-    const int64_t c0 = column<VEC>(j, 0, t, threads);
-    if (VEC && c0 + 8 <= cols) {
-        uint32_t w[2];
+// Rows of q start on 16 bytes, so a piece is 8 bytes on a boundary of 8.
+template <bool SHIFT>
+__device__ __forceinline__ void store8_bytes(int8_t* row, int c, int cols, uint32_t lo, uint32_t hi) {
+    if (SHIFT && (threadIdx.x & 31) == 0) return;
+    if (c >= 0 && c + 8 <= cols) {
+        *reinterpret_cast<uint2*>(row + c) = make_uint2(lo, hi);
+    } else {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            w[i] = __byte_perm(__byte_perm(q[4 * i], q[4 * i + 1], 0x0040), __byte_perm(q[4 * i + 2], q[4 * i + 3], 0x0040), 0x5410);
-        *reinterpret_cast<uint2*>(row + c0) = make_uint2(w[0], w[1]);
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int64_t c = column<VEC>(j, e, t, threads);
-        if (c < cols) row[c] = (int8_t)q[e];
+        for (int e = 0; e < 8; ++e)
+            if (c + e >= 0 && c + e < cols) row[c + e] = (int8_t)((e < 4 ? lo : hi) >> (8 * (e & 3)));
     }
 }
 
-// Sum of `a`, sum of `b` and maximum of `m` over the threads of a row (a warp, or a block).  `scratch`: 3 * 33 words,
-// free for the next row after one more barrier.
-template <bool WARP, bool TWO>
-__device__ __forceinline__ void row_reduce(float& a, float& b, uint32_t& m, uint32_t* scratch) {
-#pragma unroll
-    for (int d = 16; d; d >>= 1) {
-        a += __shfl_xor_sync(kFullMask, a, d);
-        if (TWO) b += __shfl_xor_sync(kFullMask, b, d);
+// ---- reductions over a team -------------------------------------------------------------------------------------
+struct Team {
+    int warps, warp, id;  // id: of the team in its block
+    __device__ __forceinline__ void sync() const {
+        if (warps > 1) asm volatile("bar.sync %0, %1;" ::"r"(id + 1), "r"(warps * 32) : "memory");
     }
-    m = __reduce_max_sync(kFullMask, m);
-    if (WARP || blockDim.x == 32) return;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    if (lane == 0) scratch[warp] = __float_as_uint(a), scratch[33 + warp] = m, scratch[66 + warp] = __float_as_uint(b);
-    __syncthreads();
-    a = lane < warps ? __uint_as_float(scratch[lane]) : 0.0f;
-    b = TWO && lane < warps ? __uint_as_float(scratch[66 + lane]) : 0.0f;
-    m = lane < warps ? scratch[33 + lane] : 0u;
+};
+
+// Sum of `a`, sum of `b` and maximum of `m` over a team.  `scratch`: 3 * 32 words of the team, free for another use
+// after one more barrier.
+template <bool A, bool B, bool M>
+__device__ __forceinline__ void team_reduce(const Team& team, float& a, float& b, uint32_t& m, uint32_t* scratch) {
+    const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int d = 16; d; d >>= 1) {
-        a += __shfl_xor_sync(kFullMask, a, d);
-        if (TWO) b += __shfl_xor_sync(kFullMask, b, d);
+    for (int round = 0; round < 2; ++round) {
+#pragma unroll
+        for (int d = 16; d; d >>= 1) {
+            if (A) a += __shfl_xor_sync(kFullMask, a, d);
+            if (B) b += __shfl_xor_sync(kFullMask, b, d);
+        }
+        if (M) m = __reduce_max_sync(kFullMask, m);
+        if (round || team.warps == 1) return;
+        if (lane == 0) {
+            if (A) scratch[team.warp] = __float_as_uint(a);
+            if (B) scratch[32 + team.warp] = __float_as_uint(b);
+            if (M) scratch[64 + team.warp] = m;
+        }
+        team.sync();
+        const bool in = lane < team.warps;
+        if (A) a = in ? __uint_as_float(scratch[lane]) : 0.0f;
+        if (B) b = in ? __uint_as_float(scratch[32 + lane]) : 0.0f;
+        if (M) m = in ? scratch[64 + lane] : 0u;
     }
-    m = __reduce_max_sync(kFullMask, m);
 }
 
+// ---- quantisation -------------------------------------------------------------------------------------------------
 enum RowOp { kPlain, kGate, kNorm };
 
 struct QuantArgs {
@@ -152,39 +250,9 @@ struct QuantArgs {
     float eps;
 };
 
-__device__ __forceinline__ float sigmoid(float g) { return 1.0f / (1.0f + __expf(-g)); }
-
-// What a row consists of: piece j of v (the values to be quantised up to a factor of the row), h on the way.
-template <int OP, int DT, bool VEC>
-__device__ __forceinline__ void row_piece(const QuantArgs& a, int64_t r, int64_t j, int t, int threads, float (&v)[8], float (&h)[8]) {
-    typedef typename Store<DT>::type T;
-    load8<VEC>(static_cast<const T*>(a.x) + r * a.ldx, j, t, threads, a.cols, h);
-    if (OP == kPlain) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = h[e];
-    } else if (OP == kGate) {
-        float u[8];
-        load8<VEC>(static_cast<const T*>(a.x2) + r * a.ldx2, j, t, threads, a.cols, u);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = h[e] * sigmoid(h[e]) * u[e];
-    } else {
-        if (a.x2) {
-            float s[8];
-            load8<VEC>(static_cast<const T*>(a.x2) + r * a.ldx2, j, t, threads, a.cols, s);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) h[e] += s[e];
-        }
-        if (a.weight) {
-            float w[8];
-            load8<VEC>(a.weight, j, t, threads, a.cols, w);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = h[e] * w[e];
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = h[e];
-        }
-    }
-}
+// 1 / (1 + exp(-g)) to a few units of the last place; the approximate quotient is 0 where 1 + exp(-g) passes 2^126, that is
+// below g = -87.3, where the sigmoid is under 2^-125.
+__device__ __forceinline__ float sigmoid(float g) { return __fdividef(1.0f, 1.0f + __expf(-g)); }
 
 // The factor that turns v into steps of the row, and the step itself.
 struct RowScale {
@@ -193,98 +261,177 @@ struct RowScale {
 __device__ __forceinline__ RowScale row_scale(uint32_t top_bits, float factor) {
     RowScale s{1.0f, 0.0f, 0.0f};
     const float top = __uint_as_float(top_bits);
-    if (top_bits >= kInfBits || __float_as_uint(fabsf(factor)) >= kInfBits) {
-        s.scale = __uint_as_float(0x7FC00000u);
+    if (top_bits >= kInfBits) {
+        s.scale = __uint_as_float(kNanBits);
     } else if (top_bits) {
         // 127 / top is out of range for a tiny top: the row is brought up by a power of two first (exact)
         if (top < 0x1p-100f) s.pre = 0x1p100f;
         s.inv = 127.0f / (top * s.pre);
         s.scale = top * factor / 127.0f;
-        if (__float_as_uint(s.scale) >= kInfBits) s.scale = __uint_as_float(0x7FC00000u), s.inv = 0.0f;
+        if (__float_as_uint(s.scale) >= kInfBits) s.scale = __uint_as_float(kNanBits), s.inv = 0.0f;
     }
     return s;
 }
 
-template <bool VEC>
-__device__ __forceinline__ void store_quantized(const QuantArgs& a, int64_t r, int64_t j, int t, int threads, const float (&v)[8], const RowScale& s) {
-    int q[8];
+// v * inv is rounded to a whole number by adding 1.5 * 2^23 in one fused step: the sum's low byte is the number in two's
+// complement (|v * inv| stays below 127.5).  A row without a finite non-zero step gets zeros.
+template <bool SHIFT>
+__device__ __forceinline__ void store_quantized(const QuantArgs& a, int64_t r, int c, float (&v)[8], const RowScale& s) {
+    constexpr float kRound = 12582912.0f;
+    uint32_t b[8];
+    if (s.inv == 0.0f) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) q[e] = s.inv == 0.0f ? 0 : __float2int_rn(v[e] * s.pre * s.inv);
-    store8_int<VEC>(a.q + r * a.ldq, j, t, threads, a.cols, q);
+        for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+    }
+    if (s.pre != 1.0f) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= s.pre;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) b[e] = __float_as_uint(fmaf(v[e], s.inv, kRound));
+    const uint32_t lo = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+    const uint32_t hi = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410);
+    store8_bytes<SHIFT>(a.q + r * a.ldq, c, (int)a.cols, lo, hi);
     if (a.values) {
         float z[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) z[e] = (float)q[e] * s.scale;
-        store8<VEC>(a.values + r * a.ldv, j, t, threads, a.cols, z);
+        for (int e = 0; e < 8; ++e) z[e] = (__uint_as_float(b[e]) - kRound) * s.scale;
+        store8<SHIFT>(a.values + r * a.ldv, c, (int)a.cols, z);
     }
 }
 
-// blockDim.x threads a row; WARP: 32 of them, blockDim.y rows a block.
-template <int OP, int DT, bool VEC, bool WARP, int NV>
-__global__ void __launch_bounds__(WARP ? 32 * kWarpRows : kMaxRowThreads) k_rows_quantize(const QuantArgs a) {
+// blockDim: (32 * warps of a team, teams)
+template <int OP, int DT, bool SHIFT, int NV>
+__global__ void __launch_bounds__(32 * quantize_warps(NV)) k_rows_quantize(const QuantArgs a) {
     typedef typename Store<DT>::type T;
-    __shared__ uint32_t scratch[99];
-    const int t = threadIdx.x, threads = WARP ? 32 : blockDim.x;
-    const int64_t r = WARP ? (int64_t)blockIdx.x * blockDim.y + threadIdx.y : blockIdx.x;
-    if (WARP && r >= a.rows) return;
-    float sum = 0.0f, unused = 0.0f;
-    uint32_t top = 0;
+    __shared__ uint32_t s_scratch[kBlockWarps][96];
+    const Team team{(int)(blockDim.x >> 5), (int)(threadIdx.x >> 5), (int)threadIdx.y};
+    const Lanes<SHIFT> at{team.warps, team.warp, (int)(threadIdx.x & 31)};
+    const int64_t r = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+    if (r >= a.rows) return;  // (a whole team)
+    const int cols = (int)a.cols;
+    const T* x = static_cast<const T*>(a.x) + r * a.ldx;
+    const T* x2 = static_cast<const T*>(a.x2) + r * a.ldx2;
+    T* h = static_cast<T*>(a.h) + r * a.ldh;
     constexpr int kHeld = NV ? NV : 1;
-    float v[kHeld][8];
-    const int64_t pieces = NV ? NV : (a.cols + 8 * threads - 1) / (8 * threads);
-    auto take = [&](int64_t j, float (&p)[8]) {
-        float h[8];
-        row_piece<OP, DT, VEC>(a, r, j, t, threads, p, h);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if (OP == kNorm) sum = fmaf(h[e], h[e], sum);
-            top = max(top, __float_as_uint(fabsf(p[e])));
-        }
-        // (the first walk over a row that is read twice leaves h alone: it may be x or the residual itself)
-        if (OP == kNorm && NV && a.h) store8<VEC>(static_cast<T*>(a.h) + r * a.ldh, j, t, threads, a.cols, h);
+    const int rounds = (row_pieces<SHIFT>(cols) + team.warps * at.kPieces - 1) / (team.warps * at.kPieces);
+    float v[kHeld][8], sum = 0.0f, unused = 0.0f;
+    uint32_t top = 0;
+    // a piece of x + residual, or of silu(gate) * up
+    const bool two = OP == kGate || (OP == kNorm && a.x2);
+    auto fetch = [&](int c, Piece<SHIFT, T>& p, Piece<SHIFT, T>& p2) {
+        p.fetch(x, c, cols);
+        if (two) p2.fetch(x2, c, cols);
     };
-    if (NV) {
+    auto get = [&](int c, const Piece<SHIFT, T>& p, const Piece<SHIFT, T>& p2, float (&o)[8]) {
+        p.get(x, c, cols, o);
+        if (two) {
+            float u[8];
+            p2.get(x2, c, cols, u);
 #pragma unroll
-        for (int j = 0; j < kHeld; ++j) take(j, v[j]);
+            for (int e = 0; e < 8; ++e) o[e] = OP == kGate ? o[e] * sigmoid(o[e]) * u[e] : o[e] + u[e];
+        }
+    };
+    auto weigh = [&](int c, float (&p)[8]) {
+        if (OP == kNorm && a.weight) {
+            float w[8];
+            load8<SHIFT>(a.weight, c, cols, w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p[e] *= w[e];
+        }
+    };
+    auto squares = [&](const float (&p)[8]) {
+        if (OP == kNorm && at.counted()) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum = fmaf(p[e], p[e], sum);
+        }
+    };
+    auto largest = [&](const float (&p)[8]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(fabsf(p[e])));
+    };
+    if constexpr (NV != 0) {
+        Piece<SHIFT, T> p[kHeld], p2[kHeld];
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j) fetch(at.column(j), p[j], p2[j]);
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j) get(at.column(j), p[j], p2[j], v[j]), squares(v[j]);
+        if (OP == kNorm && a.h) {
+            // (SHIFT: a lane stores columns of the lane before it, which has fetched them first where h is x or the residual)
+            if (SHIFT && (a.h == a.x || a.h == a.x2)) team.sync();
+#pragma unroll
+            for (int j = 0; j < kHeld; ++j) store8<SHIFT>(h, at.column(j), cols, v[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j) weigh(at.column(j), v[j]), largest(v[j]);
     } else {
-        for (int64_t j = 0; j < pieces; ++j) take(j, v[0]);
+        for (int j = 0; j < rounds; ++j) {
+            Piece<SHIFT, T> p, p2;
+            fetch(at.column(j), p, p2);
+            get(at.column(j), p, p2, v[0]);
+            squares(v[0]);
+            weigh(at.column(j), v[0]);
+            largest(v[0]);
+        }
     }
-    row_reduce<WARP, false>(sum, unused, top, scratch);
-    const float factor = OP == kNorm ? 1.0f / sqrtf(sum / (float)a.cols + a.eps) : 1.0f;
-    const bool lost = OP == kNorm && __float_as_uint(sum) >= kInfBits;
-    const RowScale s = row_scale(lost ? kInfBits : top, factor);
-    if (t == 0) a.scale[r] = s.scale;
-    if (NV) {
+    team_reduce<OP == kNorm, false, true>(team, sum, unused, top, s_scratch[team.id]);
+    float factor = 1.0f;
+    if (OP == kNorm) {
+        factor = 1.0f / sqrtf(sum / (float)cols + a.eps);
+        if (__float_as_uint(sum) >= kInfBits) top = kInfBits;
+    }
+    const RowScale s = row_scale(top, factor);
+    if (threadIdx.x == 0) a.scale[r] = s.scale;
+    if constexpr (NV != 0) {
 #pragma unroll
-        for (int j = 0; j < kHeld; ++j) store_quantized<VEC>(a, r, j, t, threads, v[j], s);
+        for (int j = 0; j < kHeld; ++j) store_quantized<SHIFT>(a, r, at.column(j), v[j], s);
     } else {
-        for (int64_t j = 0; j < pieces; ++j) {
-            float h[8];
-            row_piece<OP, DT, VEC>(a, r, j, t, threads, v[0], h);
-            if (OP == kNorm && a.h) store8<VEC>(static_cast<T*>(a.h) + r * a.ldh, j, t, threads, a.cols, h);
-            store_quantized<VEC>(a, r, j, t, threads, v[0], s);
+        // the second walk; h is stored only now, since it may be x or the residual itself.  (SHIFT: a lane stores columns of the lane
+        // before it, so a round is stored when the whole team has fetched it and the next one.)
+        Piece<SHIFT, T> p, p2;
+        fetch(at.column(0), p, p2);
+        get(at.column(0), p, p2, v[0]);
+        for (int j = 0; j < rounds; ++j) {
+            float next[8];
+            if (j + 1 < rounds) {
+                fetch(at.column(j + 1), p, p2);
+                get(at.column(j + 1), p, p2, next);
+            }
+            if (OP == kNorm && a.h) {
+                if (SHIFT) team.sync();
+                store8<SHIFT>(h, at.column(j), cols, v[0]);
+            }
+            weigh(at.column(j), v[0]);
+            store_quantized<SHIFT>(a, r, at.column(j), v[0], s);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[0][e] = next[e];
         }
     }
 }
 
-template <int OP, int DT, bool VEC>
+// How a row is laid over a team: NV pieces a lane, `warps` of them, `teams` a block.  nv = 0: longer than max_warps hold.
+struct Shape {
+    int nv, warps, teams;
+};
+Shape row_shape(int64_t cols, bool shift, int nv, int max_warps) {
+    const int64_t lanes = shift ? 31 : 32, pieces = shift ? row_pieces<true>((int)cols) : row_pieces<false>((int)cols);
+    Shape s{nv, (int)((pieces + lanes * nv - 1) / (lanes * nv)), 1};
+    if (s.warps > max_warps) return Shape{0, 32, 1};
+    if (s.warps <= kBlockWarps) s.teams = kBlockWarps / s.warps;
+    return s;
+}
+
+template <int OP, int DT, bool SHIFT>
 void launch_quantize(const QuantArgs& a, int n_sm, cudaStream_t st) {
-    const int64_t cols = a.cols;
-    if (cols <= 1024 && a.rows > n_sm) {
-        const dim3 block(32, kWarpRows);
-        const unsigned grid = (unsigned)((a.rows + kWarpRows - 1) / kWarpRows);
-        if (cols <= 256) k_rows_quantize<OP, DT, VEC, true, 1><<<grid, block, 0, st>>>(a);
-        else if (cols <= 512) k_rows_quantize<OP, DT, VEC, true, 2><<<grid, block, 0, st>>>(a);
-        else k_rows_quantize<OP, DT, VEC, true, 4><<<grid, block, 0, st>>>(a);
-        return;
-    }
-    const unsigned grid = (unsigned)a.rows;
-    auto threads = [&](int nv) { return (int)std::max<int64_t>(1, (cols + 256 * nv - 1) / (256 * nv)) * 32; };
-    // few rows: as many threads as the row feeds; many rows: more bytes in flight per thread, more rows per SM
-    if (cols > 8 * 4 * kMaxRowThreads) k_rows_quantize<OP, DT, VEC, false, 0><<<grid, kMaxRowThreads, 0, st>>>(a);
-    else if (a.rows <= n_sm && cols <= 8 * kMaxRowThreads) k_rows_quantize<OP, DT, VEC, false, 1><<<grid, threads(1), 0, st>>>(a);
-    else if (a.rows <= n_sm && cols <= 16 * kMaxRowThreads) k_rows_quantize<OP, DT, VEC, false, 2><<<grid, threads(2), 0, st>>>(a);
-    else k_rows_quantize<OP, DT, VEC, false, 4><<<grid, threads(4), 0, st>>>(a);
+    // few rows: as many lanes as a row feeds; many rows: more bytes in flight a lane
+    Shape s{0, 0, 0};
+    for (int nv = a.rows <= n_sm ? 1 : SHIFT ? 2 : 4; nv <= 4 && s.nv == 0; nv *= 2) s = row_shape(a.cols, SHIFT, nv, quantize_warps(nv));
+    const dim3 block(32 * s.warps, s.teams);
+    const unsigned grid = (unsigned)((a.rows + s.teams - 1) / s.teams);
+    if (s.nv == 0) k_rows_quantize<OP, DT, SHIFT, 0><<<grid, block, 0, st>>>(a);
+    else if (s.nv == 1) k_rows_quantize<OP, DT, SHIFT, 1><<<grid, block, 0, st>>>(a);
+    else if (s.nv == 2) k_rows_quantize<OP, DT, SHIFT, 2><<<grid, block, 0, st>>>(a);
+    else k_rows_quantize<OP, DT, SHIFT, 4><<<grid, block, 0, st>>>(a);
 }
 
 // ---- gradients -------------------------------------------------------------------------------------------------
@@ -292,136 +439,176 @@ struct NormBackArgs {
     const void *dy, *h, *dh;  // dh nullable
     const float* weight;      // nullable
     void* dx;
-    float* part;              // [gridDim.x][cols] partial sums of dweight (nullable)
+    float* part;              // [teams of the grid][cols] partial sums of dweight (nullable)
     int64_t lddy, ldh, lddh, lddx, rows, cols;
     float eps;
 };
 
-// A block takes rows blockIdx.x, + gridDim.x, ...; a thread keeps its columns, so the partial sums of dweight stay in
-// registers (NV = 0: in the block's slice of the workspace) until the block is done.
-template <int DT, bool VEC, int NV>
-__global__ void __launch_bounds__(NV ? kBackThreads : kMaxRowThreads) k_norm_backward(const NormBackArgs a) {
+// A team takes rows in steps of the number of teams.  A lane keeps its columns, so the weights and the partial sums of
+// dweight have a fixed place in shared memory (registers are what limits the rows in flight), NV pieces of two 16-byte
+// vectors a lane; with NV = 0 the sums are in the team's slice of the workspace all along.
+template <int DT, bool SHIFT, int NV>
+__global__ void __launch_bounds__(32 * backward_warps(NV), NV == 1 ? 2 : 1) k_norm_backward(const NormBackArgs a) {
     typedef typename Store<DT>::type T;
-    __shared__ uint32_t scratch[2][99];
-    const int t = threadIdx.x, threads = blockDim.x;
+    extern __shared__ float4 s_cols[];  // weights, then sums: [NV][2][threads of the block] each
+    __shared__ uint32_t s_scratch[kBlockWarps][2][96];
+    const Team team{(int)(blockDim.x >> 5), (int)(threadIdx.x >> 5), (int)threadIdx.y};
+    const Lanes<SHIFT> at{team.warps, team.warp, (int)(threadIdx.x & 31)};
+    const int cols = (int)a.cols;
     constexpr int kHeld = NV ? NV : 1;
-    float dw[kHeld][8];
+    const int threads = blockDim.x * blockDim.y, self = threadIdx.y * blockDim.x + threadIdx.x;
+    const int64_t me = (int64_t)blockIdx.x * blockDim.y + threadIdx.y, teams = (int64_t)gridDim.x * blockDim.y;
+    if (me >= a.rows) return;  // (a whole team; it has no slice of the workspace)
+    float* part = a.part ? a.part + me * a.cols : nullptr;
+    const float inv_n = 1.0f / (float)cols;
+    auto weights = [&](int c, float (&p)[8]) {
 #pragma unroll
-    for (int j = 0; j < kHeld; ++j)
+        for (int e = 0; e < 8; ++e) p[e] = 1.0f;
+        if (a.weight) load8<SHIFT>(a.weight, c, cols, p);
+    };
+    auto kept = [&](int which, int j, float (&p)[8]) {
+        const float4 x = s_cols[((which * kHeld + j) * 2) * threads + self], y = s_cols[((which * kHeld + j) * 2 + 1) * threads + self];
+        p[0] = x.x, p[1] = x.y, p[2] = x.z, p[3] = x.w, p[4] = y.x, p[5] = y.y, p[6] = y.z, p[7] = y.w;
+    };
+    auto keep = [&](int which, int j, const float (&p)[8]) {
+        s_cols[((which * kHeld + j) * 2) * threads + self] = make_float4(p[0], p[1], p[2], p[3]);
+        s_cols[((which * kHeld + j) * 2 + 1) * threads + self] = make_float4(p[4], p[5], p[6], p[7]);
+    };
+    auto give_part = [&](int c, const float (&p)[8]) {
+        if (!at.counted()) return;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) dw[j][e] = 0.0f;
-    const int64_t pieces = NV ? NV : (a.cols + 8 * threads - 1) / (8 * threads);
-    float* part = a.part ? a.part + (int64_t)blockIdx.x * a.cols : nullptr;
+        for (int e = 0; e < 8; ++e)
+            if (c + e >= 0 && c + e < cols) part[c + e] = p[e];
+    };
+    if constexpr (NV != 0) {
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j) {
+            float p[8];
+            weights(at.column(j), p);
+            keep(0, j, p);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p[e] = 0.0f;
+            keep(1, j, p);
+        }
+    }
     int side = 0;
-    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x, side ^= 1) {
+    for (int64_t r = me; r < a.rows; r += teams, side ^= 1) {
         const T* dy = static_cast<const T*>(a.dy) + r * a.lddy;
         const T* h = static_cast<const T*>(a.h) + r * a.ldh;
         const T* dh = static_cast<const T*>(a.dh) + r * a.lddh;
         T* dx = static_cast<T*>(a.dx) + r * a.lddx;
-        float hv[kHeld][8], gv[kHeld][8];
+        float hv[kHeld][8], gv[kHeld][8], pv[kHeld][8], w[8], sum[8];
         float sq = 0.0f, along = 0.0f;
         uint32_t unused = 0;
-        auto take = [&](int64_t j, float (&hp)[8], float (&gp)[8]) {
-            load8<VEC>(h, j, t, threads, a.cols, hp);
-            load8<VEC>(dy, j, t, threads, a.cols, gp);
+        auto fetch = [&](int c, Piece<SHIFT, T> (&p)[3]) {
+            p[0].fetch(h, c, cols);
+            p[1].fetch(dy, c, cols);
+            if (a.dh) p[2].fetch(dh, c, cols);
         };
-        auto weigh = [&](int64_t j, const float (&gp)[8], float (&g)[8]) {
-            if (a.weight) {
-                float w[8];
-                load8<VEC>(a.weight, j, t, threads, a.cols, w);
+        auto get = [&](int c, const Piece<SHIFT, T> (&p)[3], float (&hp)[8], float (&gp)[8], float (&pp)[8]) {
+            p[0].get(h, c, cols, hp);
+            p[1].get(dy, c, cols, gp);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) g[e] = gp[e] * w[e];
-            } else {
+            for (int e = 0; e < 8; ++e) pp[e] = 0.0f;
+            if (a.dh) p[2].get(dh, c, cols, pp);
+        };
+        auto sums = [&](const float (&hp)[8], const float (&gp)[8]) {
+            if (!at.counted()) return;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) g[e] = gp[e];
+            for (int e = 0; e < 8; ++e) sq = fmaf(hp[e], hp[e], sq), along = fmaf(gp[e] * w[e], hp[e], along);
+        };
+        if constexpr (NV != 0) {
+            Piece<SHIFT, T> p[kHeld][3];
+#pragma unroll
+            for (int j = 0; j < kHeld; ++j) fetch(at.column(j), p[j]);
+#pragma unroll
+            for (int j = 0; j < kHeld; ++j) {
+                get(at.column(j), p[j], hv[j], gv[j], pv[j]);
+                kept(0, j, w);
+                sums(hv[j], gv[j]);
             }
-        };
-        auto sums = [&](int64_t j, const float (&hp)[8], const float (&gp)[8]) {
-            float g[8];
-            weigh(j, gp, g);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sq = fmaf(hp[e], hp[e], sq), along = fmaf(g[e], hp[e], along);
-        };
-        if (NV) {
-#pragma unroll
-            for (int j = 0; j < kHeld; ++j) take(j, hv[j], gv[j]);
-#pragma unroll
-            for (int j = 0; j < kHeld; ++j) sums(j, hv[j], gv[j]);
         } else {
-            for (int64_t j = 0; j < pieces; ++j) take(j, hv[0], gv[0]), sums(j, hv[0], gv[0]);
+            for (int j = 0; j * team.warps * at.kPieces < row_pieces<SHIFT>(cols); ++j) {
+                load8<SHIFT>(h, at.column(j), cols, hv[0]);
+                load8<SHIFT>(dy, at.column(j), cols, gv[0]);
+                weights(at.column(j), w);
+                sums(hv[0], gv[0]);
+            }
         }
-        row_reduce<false, true>(sq, along, unused, scratch[side]);  // (two buffers: a row's barrier frees the row before)
-        const float inv_n = 1.0f / (float)a.cols;
+        // (two buffers: the barrier of a row frees the buffer of the row before.  It also orders every fetch of the row before
+        // the first store to it, where dx is one of the inputs.)
+        team_reduce<true, true, false>(team, sq, along, unused, s_scratch[team.id][side]);
         const float root = 1.0f / sqrtf(sq * inv_n + a.eps);
         const float coef = along * root * inv_n;
-        auto give = [&](int64_t j, const float (&hp)[8], const float (&gp)[8], float (&w)[8]) {
-            float g[8], o[8];
-            weigh(j, gp, g);
+        auto give = [&](int c, const float (&hp)[8], const float (&gp)[8], const float (&pp)[8]) {
+            float o[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float unit = hp[e] * root;
-                o[e] = root * (g[e] - unit * coef);
-                w[e] = fmaf(gp[e], unit, w[e]);
+                o[e] = fmaf(root, fmaf(gp[e], w[e], -unit * coef), pp[e]);
+                sum[e] = fmaf(gp[e], unit, sum[e]);
             }
-            if (a.dh) {
-                float p[8];
-                load8<VEC>(dh, j, t, threads, a.cols, p);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] += p[e];
-            }
-            store8<VEC>(dx, j, t, threads, a.cols, o);
+            store8<SHIFT>(dx, c, cols, o);
         };
-        if (NV) {
+        if constexpr (NV != 0) {
 #pragma unroll
-            for (int j = 0; j < kHeld; ++j) give(j, hv[j], gv[j], dw[j]);
+            for (int j = 0; j < kHeld; ++j) {
+                kept(0, j, w);
+                kept(1, j, sum);
+                give(at.column(j), hv[j], gv[j], pv[j]);
+                keep(1, j, sum);
+            }
         } else {
-            for (int64_t j = 0; j < pieces; ++j) {
-                float w[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-                take(j, hv[0], gv[0]);
-                if (part && r != blockIdx.x) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int64_t c = column<VEC>(j, e, t, threads);
-                        if (c < a.cols) w[e] = part[c];
-                    }
+            float hn[8], gn[8], pn[8];
+            Piece<SHIFT, T> p[3];
+            fetch(at.column(0), p);
+            get(at.column(0), p, hv[0], gv[0], pv[0]);
+            for (int j = 0; j * team.warps * at.kPieces < row_pieces<SHIFT>(cols); ++j) {
+                const int c = at.column(j);
+                if ((j + 1) * team.warps * at.kPieces < row_pieces<SHIFT>(cols)) {
+                    fetch(at.column(j + 1), p);
+                    get(at.column(j + 1), p, hn, gn, pn);
                 }
-                give(j, hv[0], gv[0], w);
-                if (part) {
+                if (SHIFT) team.sync();  // (as in the second walk of k_rows_quantize)
+                weights(c, w);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int64_t c = column<VEC>(j, e, t, threads);
-                        if (c < a.cols) part[c] = w[e];
-                    }
-                }
+                for (int e = 0; e < 8; ++e) sum[e] = part && r != me && c + e >= 0 && c + e < cols ? part[c + e] : 0.0f;
+                give(c, hv[0], gv[0], pv[0]);
+                if (part) give_part(c, sum);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) hv[0][e] = hn[e], gv[0][e] = gn[e], pv[0][e] = pn[e];
             }
         }
     }
-    if (NV && part) {
+    if constexpr (NV != 0) {
+        if (part) {
 #pragma unroll
-        for (int j = 0; j < kHeld; ++j)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int64_t c = column<VEC>(j, e, t, threads);
-                if (c < a.cols) part[c] = dw[j][e];
+            for (int j = 0; j < kHeld; ++j) {
+                float p[8];
+                kept(1, j, p);
+                give_part(at.column(j), p);
             }
+        }
     }
 }
 
-// dweight[c] = sum of the row groups' partial sums, in order of the groups: 32 columns by 32 runs of groups a block.
-__global__ void __launch_bounds__(1024) k_norm_weight_sum(const float* __restrict__ part, int64_t groups, int64_t cols, float* __restrict__ dweight) {
+// dweight[c] = sum of the teams' partial sums in a fixed order: 32 columns by 32 runs of teams a block.
+__global__ void __launch_bounds__(1024) k_norm_weight_sum(const float* __restrict__ part, int64_t teams, int64_t cols, float* __restrict__ dweight) {
     __shared__ float s[32][33];
     const int64_t c = (int64_t)blockIdx.x * 32 + threadIdx.x;
     float sum = 0.0f;
-    if (c < cols)
-        for (int64_t g = threadIdx.y; g < groups; g += 32) sum += part[g * cols + c];
+    if (c < cols) {
+#pragma unroll 4
+        for (int64_t g = threadIdx.y; g < teams; g += 32) sum += part[g * cols + c];
+    }
     s[threadIdx.y][threadIdx.x] = sum;
     __syncthreads();
-    if (threadIdx.y == 0 && c < cols) {
-        float all = 0.0f;
+    // warp y adds up column y of the block's 32
+    float all = s[threadIdx.x][threadIdx.y];
 #pragma unroll
-        for (int g = 0; g < 32; ++g) all += s[g][threadIdx.x];
-        dweight[c] = all;
-    }
+    for (int d = 16; d; d >>= 1) all += __shfl_xor_sync(kFullMask, all, d);
+    const int64_t out = (int64_t)blockIdx.x * 32 + threadIdx.y;
+    if (threadIdx.x == 0 && out < cols) dweight[out] = all;
 }
 
 struct GateBackArgs {
@@ -430,31 +617,60 @@ struct GateBackArgs {
     int64_t lddy, ldg, ldu, lddg, lddu, rows, cols;
 };
 
-template <int DT, bool VEC>
-__global__ void __launch_bounds__(256) k_gate_backward(const GateBackArgs a, int64_t pieces) {
+// A team works on rounds of one piece a lane: all rounds of a row (ALIAS: an output is an input, and rows do not start on 16
+// bytes, so the team fetches a round and the next before it stores the first), or those of its share of the grid.
+template <int DT, bool SHIFT, bool ALIAS>
+__global__ void __launch_bounds__(32 * kBlockWarps) k_gate_backward(const GateBackArgs a) {
     typedef typename Store<DT>::type T;
-    const int t = threadIdx.x;
-    for (int64_t i = blockIdx.x; i < a.rows * pieces; i += gridDim.x) {
-        const int64_t r = i / pieces, j = i - r * pieces;
-        float d[8], g[8], u[8], dg[8], du[8];
-        load8<VEC>(static_cast<const T*>(a.dy) + r * a.lddy, j, t, 256, a.cols, d);
-        load8<VEC>(static_cast<const T*>(a.gate) + r * a.ldg, j, t, 256, a.cols, g);
-        load8<VEC>(static_cast<const T*>(a.up) + r * a.ldu, j, t, 256, a.cols, u);
+    const Team team{(int)(blockDim.x >> 5), (int)(threadIdx.x >> 5), (int)threadIdx.y};
+    const Lanes<SHIFT> at{team.warps, team.warp, (int)(threadIdx.x & 31)};
+    const int cols = (int)a.cols;
+    const int rounds = (row_pieces<SHIFT>(cols) + team.warps * at.kPieces - 1) / (team.warps * at.kPieces);
+    for (int64_t r = (int64_t)blockIdx.x * blockDim.y + threadIdx.y; r < a.rows; r += (int64_t)gridDim.x * blockDim.y) {
+        const T* dy = static_cast<const T*>(a.dy) + r * a.lddy;
+        const T* gate = static_cast<const T*>(a.gate) + r * a.ldg;
+        const T* up = static_cast<const T*>(a.up) + r * a.ldu;
+        T* dgate = static_cast<T*>(a.dgate) + r * a.lddg;
+        T* dup = static_cast<T*>(a.dup) + r * a.lddu;
+        float d[8], g[8], u[8], dn[8], gn[8], un[8];
+        auto fetch = [&](int c, float (&dp)[8], float (&gp)[8], float (&up8)[8]) {
+            Piece<SHIFT, T> p, q, o;
+            p.fetch(dy, c, cols);
+            q.fetch(gate, c, cols);
+            o.fetch(up, c, cols);
+            p.get(dy, c, cols, dp);
+            q.get(gate, c, cols, gp);
+            o.get(up, c, cols, up8);
+        };
+        if (ALIAS) fetch(at.column(0), d, g, u);
+        for (int j = blockIdx.y; j < rounds; j += gridDim.y) {
+            const int c = at.column(j);
+            if (ALIAS) {
+                if (j + 1 < rounds) fetch(at.column(j + 1), dn, gn, un);
+                team.sync();
+            } else {
+                fetch(c, d, g, u);
+            }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float s = sigmoid(g[e]);
-            dg[e] = d[e] * u[e] * s * fmaf(g[e], 1.0f - s, 1.0f);
-            du[e] = d[e] * g[e] * s;
+            for (int e = 0; e < 8; ++e) {
+                const float s = sigmoid(g[e]), ds = d[e] * s;
+                u[e] = ds * u[e] * fmaf(g[e], 1.0f - s, 1.0f);
+                d[e] = ds * g[e];
+            }
+            store8<SHIFT>(dgate, c, cols, u);
+            store8<SHIFT>(dup, c, cols, d);
+            if (ALIAS) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) d[e] = dn[e], g[e] = gn[e], u[e] = un[e];
+            }
         }
-        store8<VEC>(static_cast<T*>(a.dgate) + r * a.lddg, j, t, 256, a.cols, dg);
-        store8<VEC>(static_cast<T*>(a.dup) + r * a.lddu, j, t, 256, a.cols, du);
     }
 }
 
 // ---- host side ---------------------------------------------------------------------------------------------------
-constexpr int64_t kMaxExtent = (int64_t)1 << 31;
+constexpr int64_t kMaxRows = ((int64_t)1 << 31) - 1, kMaxCols = (int64_t)1 << 30;  // (columns, and those past the end, in 32 bits)
 
-bool extent_ok(int64_t rows, int64_t cols) { return rows < kMaxExtent && cols < kMaxExtent; }
+bool extent_ok(int64_t rows, int64_t cols) { return rows <= kMaxRows && cols <= kMaxCols; }
 bool span_ok(int64_t rows, int64_t ld) { return rows == 0 || ld <= ((int64_t)1 << 60) / rows; }
 bool matrix_arg_ok(const void* p, int64_t ld, int64_t cols, size_t align) { return p && reinterpret_cast<uintptr_t>(p) % align == 0 && ld >= cols; }
 bool on_16(const void* p, int64_t ld, int64_t rows, size_t elem) {
@@ -503,23 +719,52 @@ dnns_status run_quantize(const QuantArgs& a, int32_t dtype, void* stream) {
     const size_t e = elem_bytes(dtype);
     const bool vec = on_16(a.x, a.ldx, a.rows, e) && (!a.x2 || on_16(a.x2, a.ldx2, a.rows, e)) && (!a.h || on_16(a.h, a.ldh, a.rows, e)) &&
                      (!a.values || on_16(a.values, a.ldv, a.rows, 2)) && (!a.weight || on_16(a.weight, 0, 1, 4));
-    if (dtype == DNNS_F32) vec ? launch_quantize<OP, DNNS_F32, true>(a, n_sm, st) : launch_quantize<OP, DNNS_F32, false>(a, n_sm, st);
-    else vec ? launch_quantize<OP, DNNS_BF16, true>(a, n_sm, st) : launch_quantize<OP, DNNS_BF16, false>(a, n_sm, st);
+    if (dtype == DNNS_F32) vec ? launch_quantize<OP, DNNS_F32, false>(a, n_sm, st) : launch_quantize<OP, DNNS_F32, true>(a, n_sm, st);
+    else vec ? launch_quantize<OP, DNNS_BF16, false>(a, n_sm, st) : launch_quantize<OP, DNNS_BF16, true>(a, n_sm, st);
     return cudaGetLastError() == cudaSuccess ? DNNS_OK : DNNS_ERR_CUDA;
 }
 
-// Blocks of the norm's gradient: bounded by the rows, and by what a machine of up to 160 SMs holds at a time; the
-// workspace is sized for it without asking the device.
-int64_t norm_backward_groups(int64_t rows) { return std::min<int64_t>(rows, 320); }
+// Teams of the norm's gradient: as many as stay busy on the 148 SMs with at least 16 rows each, so that the partial sums of
+// dweight, one row of fp32 a team, stay small beside the matrices.
+Shape norm_backward_shape(int64_t cols, bool shift) {
+    Shape s{0, 0, 0};
+    for (int nv = 1; nv <= 2 && s.nv == 0; nv *= 2) s = row_shape(cols, shift, nv, backward_warps(nv));
+    if (s.nv == 0) s.warps = backward_warps(0);
+    return s;
+}
+int64_t norm_backward_teams(int64_t rows, int64_t cols) {
+    const Shape s = norm_backward_shape(cols, true);
+    const int64_t room = 148 * std::max(1, (s.nv == 1 ? 32 : 20) / s.warps);  // (64 and 96 registers a thread)
+    return std::min(rows, std::min(room, std::max<int64_t>(148, rows / 16)));
+}
 
-template <int DT, bool VEC>
-void launch_norm_backward(const NormBackArgs& a, cudaStream_t st) {
-    const unsigned grid = (unsigned)norm_backward_groups(a.rows);
-    auto threads = [&](int nv) { return (int)((a.cols + 256 * nv - 1) / (256 * nv)) * 32; };
-    if (a.cols > 8 * 4 * kBackThreads) k_norm_backward<DT, VEC, 0><<<grid, kMaxRowThreads, 0, st>>>(a);
-    else if (a.cols <= 8 * kBackThreads) k_norm_backward<DT, VEC, 1><<<grid, threads(1), 0, st>>>(a);
-    else if (a.cols <= 16 * kBackThreads) k_norm_backward<DT, VEC, 2><<<grid, threads(2), 0, st>>>(a);
-    else k_norm_backward<DT, VEC, 4><<<grid, threads(4), 0, st>>>(a);
+template <int DT, bool SHIFT>
+bool launch_norm_backward(const NormBackArgs& a, cudaStream_t st) {
+    static std::atomic<uint64_t> done{0};
+    Shape s = norm_backward_shape(a.cols, SHIFT);
+    const int64_t teams = norm_backward_teams(a.rows, a.cols);
+    while (teams % s.teams) --s.teams;  // (every team of the grid has a slice of the workspace)
+    const unsigned grid = (unsigned)(teams / s.teams);
+    const dim3 block(32 * s.warps, s.teams);
+    const size_t shared = (size_t)s.nv * 2 * 32 * block.x * block.y;
+    if (s.nv == 0) k_norm_backward<DT, SHIFT, 0><<<grid, block, 0, st>>>(a);
+    else if (s.nv == 1) k_norm_backward<DT, SHIFT, 1><<<grid, block, shared, st>>>(a);
+    else {
+        int dev = 0;
+        if (cudaGetDevice(&dev) != cudaSuccess || !allow_shared(k_norm_backward<DT, SHIFT, 2>, 2 * 2 * 32 * 32 * backward_warps(2), done, dev)) return false;
+        k_norm_backward<DT, SHIFT, 2><<<grid, block, shared, st>>>(a);
+    }
+    return true;
+}
+
+template <int DT, bool SHIFT, bool ALIAS>
+void launch_gate_backward(const GateBackArgs& a, int n_sm, cudaStream_t st) {
+    Shape s = row_shape(a.cols, SHIFT, 1, kBlockWarps);
+    if (s.nv == 0) s = Shape{1, kBlockWarps, 1};
+    const int lanes = SHIFT ? 31 : 32;
+    const int rounds = (row_pieces<SHIFT>((int)a.cols) + lanes * s.warps - 1) / (lanes * s.warps);
+    const dim3 grid((unsigned)std::min<int64_t>((a.rows + s.teams - 1) / s.teams, (int64_t)1 << 30), ALIAS ? 1 : std::min(rounds, 65535));
+    k_gate_backward<DT, SHIFT, ALIAS><<<grid, dim3(32 * s.warps, s.teams), 0, st>>>(a);
 }
 
 bool eps_ok(float eps) { return eps >= 0x1p-126f && eps <= 3.402823466e38f; }
@@ -555,7 +800,7 @@ dnns_status dnns_silu_gate_quantize(const void* gate, int64_t ldg, const void* u
 
 size_t dnns_rmsnorm_backward_workspace_bytes(int64_t rows, int64_t cols) {
     if (rows <= 0 || cols <= 0 || !dnns::extent_ok(rows, cols)) return 0;
-    return ((size_t)dnns::norm_backward_groups(rows) * (size_t)cols * sizeof(float) + 255) & ~(size_t)255;
+    return ((size_t)dnns::norm_backward_teams(rows, cols) * (size_t)cols * sizeof(float) + 255) & ~(size_t)255;
 }
 
 dnns_status dnns_rmsnorm_backward(const void* dy, int64_t lddy, const void* h, int64_t ldh, const float* weight, float eps,
@@ -583,9 +828,10 @@ dnns_status dnns_rmsnorm_backward(const void* dy, int64_t lddy, const void* h, i
     const NormBackArgs a{dy, h, dh, weight, dx, dweight ? static_cast<float*>(ws_dev) : nullptr, lddy, ldh, lddh, lddx, rows, cols, eps};
     const bool vec = on_16(dy, lddy, rows, e) && on_16(h, ldh, rows, e) && on_16(dx, lddx, rows, e) && (!dh || on_16(dh, lddh, rows, e)) &&
                      (!weight || on_16(weight, 0, 1, 4));
-    if (dtype == DNNS_F32) vec ? launch_norm_backward<DNNS_F32, true>(a, st) : launch_norm_backward<DNNS_F32, false>(a, st);
-    else vec ? launch_norm_backward<DNNS_BF16, true>(a, st) : launch_norm_backward<DNNS_BF16, false>(a, st);
-    if (dweight) k_norm_weight_sum<<<(unsigned)((cols + 31) / 32), dim3(32, 32), 0, st>>>(a.part, norm_backward_groups(rows), cols, dweight);
+    const bool launched = dtype == DNNS_F32 ? (vec ? launch_norm_backward<DNNS_F32, false>(a, st) : launch_norm_backward<DNNS_F32, true>(a, st))
+                                            : (vec ? launch_norm_backward<DNNS_BF16, false>(a, st) : launch_norm_backward<DNNS_BF16, true>(a, st));
+    if (!launched) return DNNS_ERR_CUDA;
+    if (dweight) k_norm_weight_sum<<<(unsigned)((cols + 31) / 32), dim3(32, 32), 0, st>>>(a.part, norm_backward_teams(rows, cols), cols, dweight);
     return cudaGetLastError() == cudaSuccess ? DNNS_OK : DNNS_ERR_CUDA;
 }
 
@@ -607,11 +853,12 @@ dnns_status dnns_silu_gate_backward(const void* dy, int64_t lddy, const void* ga
     const GateBackArgs a{dy, gate, up, dgate, dup, lddy, ldg, ldu, lddg, lddu, rows, cols};
     const bool vec = on_16(dy, lddy, rows, e) && on_16(gate, ldg, rows, e) && on_16(up, ldu, rows, e) && on_16(dgate, lddg, rows, e) &&
                      on_16(dup, lddu, rows, e);
-    const int64_t pieces = (cols + 2047) / 2048;
-    const unsigned grid = (unsigned)std::min<int64_t>(rows * pieces, (int64_t)n_sm * 64);
+    bool alias = false;
+    for (const void* out : {dgate, dup}) alias = alias || out == dy || out == gate || out == up;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (dtype == DNNS_F32) vec ? k_gate_backward<DNNS_F32, true><<<grid, 256, 0, st>>>(a, pieces) : k_gate_backward<DNNS_F32, false><<<grid, 256, 0, st>>>(a, pieces);
-    else vec ? k_gate_backward<DNNS_BF16, true><<<grid, 256, 0, st>>>(a, pieces) : k_gate_backward<DNNS_BF16, false><<<grid, 256, 0, st>>>(a, pieces);
+    if (vec) dtype == DNNS_F32 ? launch_gate_backward<DNNS_F32, false, false>(a, n_sm, st) : launch_gate_backward<DNNS_BF16, false, false>(a, n_sm, st);
+    else if (alias) dtype == DNNS_F32 ? launch_gate_backward<DNNS_F32, true, true>(a, n_sm, st) : launch_gate_backward<DNNS_BF16, true, true>(a, n_sm, st);
+    else dtype == DNNS_F32 ? launch_gate_backward<DNNS_F32, true, false>(a, n_sm, st) : launch_gate_backward<DNNS_BF16, true, false>(a, n_sm, st);
     return cudaGetLastError() == cudaSuccess ? DNNS_OK : DNNS_ERR_CUDA;
 }
 
