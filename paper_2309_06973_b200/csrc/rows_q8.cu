@@ -8,13 +8,12 @@
 // r = 1 / sqrt(mean(h^2) + eps), q = rint(v * 127 / max|v|) and scale = r * max|v| / 127, so the sum of squares and the
 // maximum travel through the same shuffles and the same barrier.
 //
-// A team of warps has a row (one warp for short rows, several teams a block).  A lane works on pieces of 8 neighbouring
-// columns; NV pieces a lane, so a row of up to 8 * NV * lanes columns stays in registers, and longer ones (NV = 0) are walked
-// twice.  Rows of a rebuilt layer have any width, so they start anywhere: SHIFT handles rows that do not start on 16 bytes
-// with the same 16-byte accesses.  A lane then fetches the two aligned vectors around its piece and shifts its 8 columns
-// out of them; it stores the aligned vector that ends inside its piece, whose front columns come from the lane before it
-// by shuffles.  The first lane of a warp repeats the piece of the previous warp's last lane, so that every stored vector finds its
-// front: 31 pieces a warp instead of 32.  Only the ends of a row go element by element.
+// A team of warps has a row (a block; for short rows a warp, several a block), and a warp works on pieces of 256 columns.  Where
+// every row of every matrix starts on 16 bytes (VEC) a lane takes 8 neighbouring columns of a piece and moves them as
+// vectors.  Rows of a rebuilt layer have any width, so they start anywhere: then a lane takes every 32nd column, one element an
+// access at fixed offsets from one address; a warp still touches whole sectors, and the accesses are fewer
+// instructions than shifting misaligned vectors into place would be.  NV pieces a warp: a row of up to 256 * NV * warps columns
+// stays in registers, and longer ones (NV = 0) are walked twice.  All loads of a row are issued before the first is used.
 #include <algorithm>
 
 #include "dnns_internal.cuh"
@@ -26,10 +25,10 @@ namespace {
 constexpr uint32_t kFullMask = 0xFFFFFFFFu;
 constexpr uint32_t kInfBits = 0x7F800000u;
 constexpr uint32_t kNanBits = 0x7FC00000u;
-constexpr int kBlockWarps = 8;  // warps of a block whose teams are small
+constexpr int kBlockWarps = 8;  // warps of a block whose teams are single warps
 // Warps of a team at most, by pieces a lane: what keeps a row in registers without spilling.
 constexpr int quantize_warps(int nv) { return nv == 4 ? 16 : 32; }
-constexpr int backward_warps(int nv) { return nv == 2 ? 20 : 16; }
+constexpr int backward_warps(int nv) { return nv == 1 ? kBlockWarps : nv == 2 ? 9 : 16; }
 
 template <int DT>
 struct Store;
@@ -42,8 +41,6 @@ struct Store<DNNS_BF16> {
     typedef uint16_t type;
 };
 
-__device__ __forceinline__ float widen(float x) { return x; }
-__device__ __forceinline__ float widen(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
 // two fp32 to two bf16, nearest even, in one word (lo in the low half)
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
     uint32_t d;
@@ -53,186 +50,173 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
 __device__ __forceinline__ void narrow(float x, float& d) { d = x; }
 __device__ __forceinline__ void narrow(float x, uint16_t& d) { d = (uint16_t)bf16_pair(x, 0.0f); }
 
-// ---- pieces of 8 columns -------------------------------------------------------------------------------------
-// Where a lane's pieces are: team of `warps`, this one being number `warp`.
-template <bool SHIFT>
-struct Lanes {
-    static constexpr int kPieces = SHIFT ? 31 : 32;  // of a warp
-    int warps, warp, lane;
-    __device__ __forceinline__ int column(int j) const { return 8 * ((j * warps + warp) * kPieces + lane - (SHIFT ? 1 : 0)); }
-    // (SHIFT: lane 0's piece is the previous warp's; its values are counted there)
-    __device__ __forceinline__ bool counted() const { return !SHIFT || lane != 0; }
-};
-// pieces of a row; SHIFT: one more, since the columns at the end may be stored by the lane after the last piece
-template <bool SHIFT>
-__host__ __device__ inline int row_pieces(int cols) { return (cols + 7) / 8 + (SHIFT ? 1 : 0); }
+// ---- pieces of 256 columns of a row, 8 of them a lane's -------------------------------------------------------------
+// The first column of a lane in piece j of warp `warp` of a team of `warps`.
+template <bool VEC>
+__device__ __forceinline__ int first_column(int j, int warps, int warp) {
+    const int lane = threadIdx.x & 31;
+    return (j * warps + warp) * 256 + (VEC ? 8 * lane : lane);
+}
+template <bool VEC>
+constexpr int kStep = VEC ? 1 : 32;  // from one of a lane's columns to the next
+// All columns of the warp's piece are inside the row (the same for all lanes).
+template <bool VEC>
+__device__ __forceinline__ bool piece_inside(int c, int cols) { return c - (VEC ? 8 : 1) * (int)(threadIdx.x & 31) + 256 <= cols; }
+// None is.
+template <bool VEC>
+__device__ __forceinline__ bool piece_outside(int c, int cols) { return c - (VEC ? 8 : 1) * (int)(threadIdx.x & 31) >= cols; }
 
-// Elements by which a row starts past a 16-byte boundary.
-template <typename T>
-__device__ __forceinline__ int row_shift(const T* row) { return (int)((reinterpret_cast<uintptr_t>(row) / sizeof(T)) & (16 / sizeof(T) - 1)); }
-
-// Words s .. of a run of words: s in 16-bit steps below 8 (bf16), in words below 4 (fp32).
-__device__ __forceinline__ void shift_out(const uint32_t (&w)[8], int s, uint32_t (&r)[4]) {
-    uint32_t t[6], u[5];
-#pragma unroll
-    for (int i = 0; i < 6; ++i) t[i] = s & 4 ? w[i + 2] : w[i];
-#pragma unroll
-    for (int i = 0; i < 5; ++i) u[i] = s & 2 ? t[i + 1] : t[i];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = __funnelshift_r(u[i], u[i + 1], 16 * (s & 1));
-}
-__device__ __forceinline__ void shift_out(const uint32_t (&w)[12], int s, uint32_t (&r)[8]) {
-    uint32_t t[9];
-#pragma unroll
-    for (int i = 0; i < 9; ++i) t[i] = s & 2 ? w[i + 2] : w[i];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = s & 1 ? t[i + 1] : t[i];
-}
-__device__ __forceinline__ void widen8(const uint32_t (&w)[4], float (&v)[8]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-}
-__device__ __forceinline__ void widen8(const uint32_t (&w)[8], float (&v)[8]) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
-}
-
-// Columns c .. c + 7 of a row; those outside it read as 0.  In two steps, so that all of a lane's loads are on their way
-// before the first of them is waited for: `fetch` issues the vector loads, predicated and without a branch, `get` shifts and
-// widens what came, and reads element by element where a vector would have left the row.
-template <bool SHIFT, typename T>
-struct Piece {
-    static constexpr int kPer = 16 / sizeof(T), kWords = 2 * sizeof(T);  // elements of a vector, words of a piece
-    uint32_t w[kWords + (SHIFT ? 4 : 0)];
-    static __device__ __forceinline__ bool whole(int c, int cols, int s) { return c >= s && c + 8 + (SHIFT && s ? kPer - s : 0) <= cols; }
+// The 8 values as they are stored: vectors, or one element a word.  Loads are asm volatile, so that they are issued
+// where they stand - all of a row's before the first of them is waited for.
+template <bool VEC, typename T>
+struct Raw {
+    static constexpr int kWords = VEC ? 2 * sizeof(T) : 8;
+    uint32_t w[kWords];
     __device__ __forceinline__ void fetch(const T* row, int c, int cols) {
-        const int s = SHIFT ? row_shift(row) : 0;
-        const bool in = whole(c, cols, s);
-        const T* p = row + (c - s);
+        const T* p = row + c;
+        if (piece_inside<VEC>(c, cols)) {
+            if constexpr (VEC) {
 #pragma unroll
-        for (int i = 0; i < kWords / 4 + (SHIFT ? 1 : 0); ++i) {
-            const bool need = in && (i < kWords / 4 || s);
-            w[4 * i] = w[4 * i + 1] = w[4 * i + 2] = w[4 * i + 3] = 0;
-            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %5, 0;\n\t@p ld.global.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
-                         : "+r"(w[4 * i]), "+r"(w[4 * i + 1]), "+r"(w[4 * i + 2]), "+r"(w[4 * i + 3])
-                         : "l"(p + i * kPer), "r"((uint32_t)need)
-                         : "memory");
+                for (int i = 0; i < kWords / 4; ++i)
+                    asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[4 * i]), "=r"(w[4 * i + 1]), "=r"(w[4 * i + 2]), "=r"(w[4 * i + 3]) : "l"(p + 16 / sizeof(T) * i) : "memory");
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) load_one(p + 32 * e, w[e]);
+            }
+            return;
         }
-    }
-    __device__ __forceinline__ void get(const T* row, int c, int cols, float (&v)[8]) const {
-        const int s = SHIFT ? row_shift(row) : 0;
-        if constexpr (SHIFT) {
-            uint32_t r[kWords];
-            shift_out(w, s, r);
-            widen8(r, v);
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = 0;
+        if (piece_outside<VEC>(c, cols)) return;
+        if constexpr (VEC) {
+            const uint32_t whole = c + 8 <= cols;
+#pragma unroll
+            for (int i = 0; i < kWords / 4; ++i)
+                asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %5, 0;\n\t@p ld.global.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+                             : "+r"(w[4 * i]), "+r"(w[4 * i + 1]), "+r"(w[4 * i + 2]), "+r"(w[4 * i + 3])
+                             : "l"(p + 16 / sizeof(T) * i), "r"(whole)
+                             : "memory");
+            if (!whole && c < cols) {  // the row's last columns
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (c + e < cols) {
+                        if constexpr (sizeof(T) == 4) w[e] = __float_as_uint(p[e]);
+                        else w[e / 2] |= (uint32_t)p[e] << (16 * (e & 1));
+                    }
+            }
         } else {
-            widen8(w, v);
-        }
-        if (!whole(c, cols, s) && c + 8 > 0 && c < cols) {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if (c + e >= 0 && c + e < cols) v[e] = widen(row[c + e]);
+                if (c + 32 * e < cols) load_one(p + 32 * e, w[e]);
         }
+    }
+    __device__ __forceinline__ float get(int e) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+        else if constexpr (VEC) return __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
+        else return __uint_as_float(w[e] << 16);
+    }
+    static __device__ __forceinline__ void load_one(const T* p, uint32_t& x) {
+        if constexpr (sizeof(T) == 4) asm volatile("ld.global.u32 %0, [%1];" : "=r"(x) : "l"(p) : "memory");
+        else asm volatile("{\n\t.reg .u16 t;\n\tld.global.u16 t, [%1];\n\tcvt.u32.u16 %0, t;\n\t}" : "=r"(x) : "l"(p) : "memory");
     }
 };
-template <bool SHIFT, typename T>
-__device__ __forceinline__ void load8(const T* row, int c, int cols, float (&v)[8]) {
-    Piece<SHIFT, T> p;
-    p.fetch(row, c, cols);
-    p.get(row, c, cols, v);
+template <bool VEC>
+__device__ __forceinline__ void load8(const float* row, int c, int cols, float (&v)[8]) {
+    Raw<VEC, float> r;
+    r.fetch(row, c, cols);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = r.get(e);
 }
 
-// Stores columns c .. c + 7.  All lanes of the warp take part (SHIFT: a lane may store columns of the lane before it).
-template <bool SHIFT, typename T>
+template <bool VEC, typename T>
 __device__ __forceinline__ void store8(T* row, int c, int cols, const float (&v)[8]) {
-    constexpr int kPer = 16 / sizeof(T), kWords = 2 * sizeof(T);
-    uint32_t w[kWords + 4];  // behind the 4 words (SHIFT) of the lane before
-    if constexpr (sizeof(T) == 4) {
+    T* p = row + c;
+    if (VEC ? c + 8 <= cols : piece_inside<VEC>(c, cols)) {
+        if constexpr (!VEC) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[4 + i] = __float_as_uint(v[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[4 + i] = bf16_pair(v[2 * i], v[2 * i + 1]);
-    }
-    const int s = SHIFT ? row_shift(row) : 0;
-    if (s == 0) {
-        if (SHIFT && (threadIdx.x & 31) == 0) return;  // the previous warp's
-        if (c >= 0 && c + 8 <= cols) {
-#pragma unroll
-            for (int i = 0; i < kWords / 4; ++i) *reinterpret_cast<uint4*>(row + c + i * kPer) = make_uint4(w[4 + 4 * i], w[5 + 4 * i], w[6 + 4 * i], w[7 + 4 * i]);
+            for (int e = 0; e < 8; ++e) narrow(v[e], p[32 * e]);
+        } else if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+            *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
         } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (c + e >= 0 && c + e < cols) narrow(v[e], row[c + e]);
+            *reinterpret_cast<uint4*>(p) = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
         }
         return;
     }
-    if constexpr (SHIFT) {
+    if (piece_outside<VEC>(c, cols)) return;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = __shfl_up_sync(kFullMask, w[kWords + i], 1);
-        if ((threadIdx.x & 31) == 0) return;
-        uint32_t r[kWords];
-        shift_out(w, kPer - s, r);  // columns c - s ..
-        c -= s;
-        if (c >= 0 && c + 8 <= cols) {
-#pragma unroll
-            for (int i = 0; i < kWords / 4; ++i) *reinterpret_cast<uint4*>(row + c + i * kPer) = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+    for (int e = 0; e < 8; ++e)
+        if (c + kStep<VEC> * e < cols) narrow(v[e], p[kStep<VEC> * e]);
+}
+// The low bytes of 8 words.
+template <bool VEC>
+__device__ __forceinline__ void store8_bytes(int8_t* row, int c, int cols, const uint32_t (&b)[8]) {
+    int8_t* p = row + c;
+    if (VEC ? c + 8 <= cols : piece_inside<VEC>(c, cols)) {
+        if constexpr (VEC) {
+            const uint32_t lo = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+            const uint32_t hi = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410);
+            *reinterpret_cast<uint2*>(p) = make_uint2(lo, hi);
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (c + e >= 0 && c + e < cols) {
-                    if constexpr (sizeof(T) == 4) row[c + e] = __uint_as_float(r[e]);
-                    else row[c + e] = (uint16_t)(r[e / 2] >> (16 * (e & 1)));
-                }
+            for (int e = 0; e < 8; ++e) p[32 * e] = (int8_t)b[e];
         }
+        return;
     }
-}
-
-// Rows of q start on 16 bytes, so a piece is 8 bytes on a boundary of 8.
-template <bool SHIFT>
-__device__ __forceinline__ void store8_bytes(int8_t* row, int c, int cols, uint32_t lo, uint32_t hi) {
-    if (SHIFT && (threadIdx.x & 31) == 0) return;
-    if (c >= 0 && c + 8 <= cols) {
-        *reinterpret_cast<uint2*>(row + c) = make_uint2(lo, hi);
-    } else {
+    if (piece_outside<VEC>(c, cols)) return;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (c + e >= 0 && c + e < cols) row[c + e] = (int8_t)((e < 4 ? lo : hi) >> (8 * (e & 3)));
-    }
+    for (int e = 0; e < 8; ++e)
+        if (c + kStep<VEC> * e < cols) p[kStep<VEC> * e] = (int8_t)b[e];
 }
 
-// ---- reductions over a team -------------------------------------------------------------------------------------
-struct Team {
-    int warps, warp, id;  // id: of the team in its block
-    __device__ __forceinline__ void sync() const {
-        if (warps > 1) asm volatile("bar.sync %0, %1;" ::"r"(id + 1), "r"(warps * 32) : "memory");
-    }
-};
-
-// Sum of `a`, sum of `b` and maximum of `m` over a team.  `scratch`: 3 * 32 words of the team, free for another use
-// after one more barrier.
-template <bool A, bool B, bool M>
-__device__ __forceinline__ void team_reduce(const Team& team, float& a, float& b, uint32_t& m, uint32_t* scratch) {
-    const int lane = threadIdx.x & 31;
+// ---- reductions over a team: a warp (warps = 1), or the block ----------------------------------------------------
+// Sum of `a` and maximum of `m`.  `scratch`: 64 words, free for another use after one more barrier.
+template <bool SUM>
+__device__ __forceinline__ void reduce_sum_max(int warps, float& a, uint32_t& m, uint32_t* scratch) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
     for (int round = 0; round < 2; ++round) {
+        if (SUM) {
 #pragma unroll
-        for (int d = 16; d; d >>= 1) {
-            if (A) a += __shfl_xor_sync(kFullMask, a, d);
-            if (B) b += __shfl_xor_sync(kFullMask, b, d);
+            for (int d = 16; d; d >>= 1) a += __shfl_xor_sync(kFullMask, a, d);
         }
-        if (M) m = __reduce_max_sync(kFullMask, m);
-        if (round || team.warps == 1) return;
+        m = __reduce_max_sync(kFullMask, m);
+        if (round || warps == 1) return;
         if (lane == 0) {
-            if (A) scratch[team.warp] = __float_as_uint(a);
-            if (B) scratch[32 + team.warp] = __float_as_uint(b);
-            if (M) scratch[64 + team.warp] = m;
+            if (SUM) scratch[warp] = __float_as_uint(a);
+            scratch[32 + warp] = m;
         }
-        team.sync();
-        const bool in = lane < team.warps;
-        if (A) a = in ? __uint_as_float(scratch[lane]) : 0.0f;
-        if (B) b = in ? __uint_as_float(scratch[32 + lane]) : 0.0f;
-        if (M) m = in ? scratch[64 + lane] : 0u;
+        __syncthreads();
+        if (SUM) a = lane < warps ? __uint_as_float(scratch[lane]) : 0.0f;
+        m = lane < warps ? scratch[32 + lane] : 0u;
+    }
+}
+
+// Sums of `a` and `b` over up to 16 warps: the lower half of a warp adds up a, the upper half b, and after the barrier everybody
+// adds up the warps' sums.
+__device__ __forceinline__ void reduce_two_sums(int warps, float& a, float& b, float2 (&scratch)[16]) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const bool upper = lane >= 16;
+    float x = upper ? b : a;
+    x += __shfl_xor_sync(kFullMask, upper ? a : b, 16);
+#pragma unroll
+    for (int d = 8; d; d >>= 1) x += __shfl_xor_sync(kFullMask, x, d);
+    if (warps == 1) {
+        a = __shfl_sync(kFullMask, x, 0);
+        b = __shfl_sync(kFullMask, x, 16);
+        return;
+    }
+    if (lane == 0) scratch[warp].x = x;
+    if (lane == 16) scratch[warp].y = x;
+    if (warp == 0 && lane >= warps && lane < 16) scratch[lane] = make_float2(0.0f, 0.0f);
+    __syncthreads();
+    a = b = 0.0f;
+    const float4* two = reinterpret_cast<const float4*>(scratch);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (2 * i >= warps) break;
+        const float4 v = two[i];
+        a += v.x + v.z, b += v.y + v.w;
     }
 }
 
@@ -250,9 +234,14 @@ struct QuantArgs {
     float eps;
 };
 
-// 1 / (1 + exp(-g)) to a few units of the last place; the approximate quotient is 0 where 1 + exp(-g) passes 2^126, that is
-// below g = -87.3, where the sigmoid is under 2^-125.
-__device__ __forceinline__ float sigmoid(float g) { return __fdividef(1.0f, 1.0f + __expf(-g)); }
+// 1 / (1 + exp(-g)) to a few units of the last place.  Below g = -87.3, where 1 + exp(-g) passes 2^126, it is 0 (the sigmoid
+// is under 2^-125 there).
+__device__ __forceinline__ float sigmoid(float g) {
+    float e, s;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(g * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(1.0f + e));
+    return s;
+}
 
 // The factor that turns v into steps of the row, and the step itself.
 struct RowScale {
@@ -275,7 +264,7 @@ __device__ __forceinline__ RowScale row_scale(uint32_t top_bits, float factor) {
 
 // v * inv is rounded to a whole number by adding 1.5 * 2^23 in one fused step: the sum's low byte is the number in two's
 // complement (|v * inv| stays below 127.5).  A row without a finite non-zero step gets zeros.
-template <bool SHIFT>
+template <bool VEC>
 __device__ __forceinline__ void store_quantized(const QuantArgs& a, int64_t r, int c, float (&v)[8], const RowScale& s) {
     constexpr float kRound = 12582912.0f;
     uint32_t b[8];
@@ -289,61 +278,52 @@ __device__ __forceinline__ void store_quantized(const QuantArgs& a, int64_t r, i
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) b[e] = __float_as_uint(fmaf(v[e], s.inv, kRound));
-    const uint32_t lo = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
-    const uint32_t hi = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410);
-    store8_bytes<SHIFT>(a.q + r * a.ldq, c, (int)a.cols, lo, hi);
+    store8_bytes<VEC>(a.q + r * a.ldq, c, (int)a.cols, b);
     if (a.values) {
         float z[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) z[e] = (__uint_as_float(b[e]) - kRound) * s.scale;
-        store8<SHIFT>(a.values + r * a.ldv, c, (int)a.cols, z);
+        store8<VEC>(a.values + r * a.ldv, c, (int)a.cols, z);
     }
 }
 
-// blockDim: (32 * warps of a team, teams)
-template <int OP, int DT, bool SHIFT, int NV>
+// blockDim: (32 * warps of a team, teams); more than one team only of one warp
+template <int OP, int DT, bool VEC, int NV>
 __global__ void __launch_bounds__(32 * quantize_warps(NV)) k_rows_quantize(const QuantArgs a) {
     typedef typename Store<DT>::type T;
-    __shared__ uint32_t s_scratch[kBlockWarps][96];
-    const Team team{(int)(blockDim.x >> 5), (int)(threadIdx.x >> 5), (int)threadIdx.y};
-    const Lanes<SHIFT> at{team.warps, team.warp, (int)(threadIdx.x & 31)};
+    __shared__ uint32_t s_scratch[64];
+    const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5;
     const int64_t r = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
     if (r >= a.rows) return;  // (a whole team)
     const int cols = (int)a.cols;
+    auto column = [&](int j) { return first_column<VEC>(j, warps, warp); };
     const T* x = static_cast<const T*>(a.x) + r * a.ldx;
     const T* x2 = static_cast<const T*>(a.x2) + r * a.ldx2;
     T* h = static_cast<T*>(a.h) + r * a.ldh;
     constexpr int kHeld = NV ? NV : 1;
-    const int rounds = (row_pieces<SHIFT>(cols) + team.warps * at.kPieces - 1) / (team.warps * at.kPieces);
-    float v[kHeld][8], sum = 0.0f, unused = 0.0f;
+    float v[kHeld][8], sum = 0.0f;
     uint32_t top = 0;
-    // a piece of x + residual, or of silu(gate) * up
     const bool two = OP == kGate || (OP == kNorm && a.x2);
-    auto fetch = [&](int c, Piece<SHIFT, T>& p, Piece<SHIFT, T>& p2) {
+    auto fetch = [&](int c, Raw<VEC, T>& p, Raw<VEC, T>& p2) {
         p.fetch(x, c, cols);
         if (two) p2.fetch(x2, c, cols);
     };
-    auto get = [&](int c, const Piece<SHIFT, T>& p, const Piece<SHIFT, T>& p2, float (&o)[8]) {
-        p.get(x, c, cols, o);
-        if (two) {
-            float u[8];
-            p2.get(x2, c, cols, u);
+    // x + residual, or silu(gate) * up
+    auto get = [&](const Raw<VEC, T>& p, const Raw<VEC, T>& p2, float (&o)[8]) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = OP == kGate ? o[e] * sigmoid(o[e]) * u[e] : o[e] + u[e];
+        for (int e = 0; e < 8; ++e) {
+            o[e] = p.get(e);
+            if (OP == kGate) o[e] = o[e] * sigmoid(o[e]) * p2.get(e);
+            if (OP == kNorm && two) o[e] += p2.get(e);
+            if (OP == kNorm) sum = fmaf(o[e], o[e], sum);
         }
     };
     auto weigh = [&](int c, float (&p)[8]) {
         if (OP == kNorm && a.weight) {
             float w[8];
-            load8<SHIFT>(a.weight, c, cols, w);
+            load8<VEC>(a.weight, c, cols, w);
 #pragma unroll
             for (int e = 0; e < 8; ++e) p[e] *= w[e];
-        }
-    };
-    auto squares = [&](const float (&p)[8]) {
-        if (OP == kNorm && at.counted()) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum = fmaf(p[e], p[e], sum);
         }
     };
     auto largest = [&](const float (&p)[8]) {
@@ -351,264 +331,354 @@ __global__ void __launch_bounds__(32 * quantize_warps(NV)) k_rows_quantize(const
         for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(fabsf(p[e])));
     };
     if constexpr (NV != 0) {
-        Piece<SHIFT, T> p[kHeld], p2[kHeld];
+        Raw<VEC, T> p[kHeld], p2[kHeld];
 #pragma unroll
-        for (int j = 0; j < kHeld; ++j) fetch(at.column(j), p[j], p2[j]);
+        for (int j = 0; j < kHeld; ++j) fetch(column(j), p[j], p2[j]);
 #pragma unroll
-        for (int j = 0; j < kHeld; ++j) get(at.column(j), p[j], p2[j], v[j]), squares(v[j]);
+        for (int j = 0; j < kHeld; ++j) get(p[j], p2[j], v[j]);
         if (OP == kNorm && a.h) {
-            // (SHIFT: a lane stores columns of the lane before it, which has fetched them first where h is x or the residual)
-            if (SHIFT && (a.h == a.x || a.h == a.x2)) team.sync();
 #pragma unroll
-            for (int j = 0; j < kHeld; ++j) store8<SHIFT>(h, at.column(j), cols, v[j]);
+            for (int j = 0; j < kHeld; ++j) store8<VEC>(h, column(j), cols, v[j]);
         }
 #pragma unroll
-        for (int j = 0; j < kHeld; ++j) weigh(at.column(j), v[j]), largest(v[j]);
+        for (int j = 0; j < kHeld; ++j) weigh(column(j), v[j]), largest(v[j]);
     } else {
-        for (int j = 0; j < rounds; ++j) {
-            Piece<SHIFT, T> p, p2;
-            fetch(at.column(j), p, p2);
-            get(at.column(j), p, p2, v[0]);
-            squares(v[0]);
-            weigh(at.column(j), v[0]);
+        for (int j = 0; column(j) < cols; ++j) {
+            Raw<VEC, T> p, p2;
+            fetch(column(j), p, p2);
+            get(p, p2, v[0]);
+            weigh(column(j), v[0]);
             largest(v[0]);
         }
+        __syncwarp();
     }
-    team_reduce<OP == kNorm, false, true>(team, sum, unused, top, s_scratch[team.id]);
+    reduce_sum_max<OP == kNorm>(warps, sum, top, s_scratch);
     float factor = 1.0f;
     if (OP == kNorm) {
-        factor = 1.0f / sqrtf(sum / (float)cols + a.eps);
+        factor = rsqrtf(sum / (float)cols + a.eps);
         if (__float_as_uint(sum) >= kInfBits) top = kInfBits;
     }
     const RowScale s = row_scale(top, factor);
     if (threadIdx.x == 0) a.scale[r] = s.scale;
     if constexpr (NV != 0) {
 #pragma unroll
-        for (int j = 0; j < kHeld; ++j) store_quantized<SHIFT>(a, r, at.column(j), v[j], s);
+        for (int j = 0; j < kHeld; ++j) store_quantized<VEC>(a, r, column(j), v[j], s);
     } else {
-        // the second walk; h is stored only now, since it may be x or the residual itself.  (SHIFT: a lane stores columns of the lane
-        // before it, so a round is stored when the whole team has fetched it and the next one.)
-        Piece<SHIFT, T> p, p2;
-        fetch(at.column(0), p, p2);
-        get(at.column(0), p, p2, v[0]);
-        for (int j = 0; j < rounds; ++j) {
-            float next[8];
-            if (j + 1 < rounds) {
-                fetch(at.column(j + 1), p, p2);
-                get(at.column(j + 1), p, p2, next);
-            }
-            if (OP == kNorm && a.h) {
-                if (SHIFT) team.sync();
-                store8<SHIFT>(h, at.column(j), cols, v[0]);
-            }
-            weigh(at.column(j), v[0]);
-            store_quantized<SHIFT>(a, r, at.column(j), v[0], s);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[0][e] = next[e];
+        // the second walk; h is stored only now, since it may be x or the residual itself
+        for (int j = 0; column(j) < cols; ++j) {
+            Raw<VEC, T> p, p2;
+            fetch(column(j), p, p2);
+            get(p, p2, v[0]);
+            if (OP == kNorm && a.h) store8<VEC>(h, column(j), cols, v[0]);
+            weigh(column(j), v[0]);
+            store_quantized<VEC>(a, r, column(j), v[0], s);
         }
     }
 }
 
-// How a row is laid over a team: NV pieces a lane, `warps` of them, `teams` a block.  nv = 0: longer than max_warps hold.
+// How a row is laid over a team: NV pieces a warp, `warps` of them, `teams` a block.  nv = 0: longer than max_warps hold.
 struct Shape {
     int nv, warps, teams;
 };
-Shape row_shape(int64_t cols, bool shift, int nv, int max_warps) {
-    const int64_t lanes = shift ? 31 : 32, pieces = shift ? row_pieces<true>((int)cols) : row_pieces<false>((int)cols);
-    Shape s{nv, (int)((pieces + lanes * nv - 1) / (lanes * nv)), 1};
-    if (s.warps > max_warps) return Shape{0, 32, 1};
-    if (s.warps <= kBlockWarps) s.teams = kBlockWarps / s.warps;
+Shape row_shape(int64_t cols, int nv, int max_warps) {
+    Shape s{nv, (int)((cols + 256 * nv - 1) / (256 * nv)), 1};
+    if (s.warps > max_warps) return Shape{0, max_warps, 1};
+    if (s.warps == 1) s.teams = kBlockWarps;
     return s;
 }
 
-template <int OP, int DT, bool SHIFT>
+template <int OP, int DT, bool VEC>
 void launch_quantize(const QuantArgs& a, int n_sm, cudaStream_t st) {
-    // few rows: as many lanes as a row feeds; many rows: more bytes in flight a lane
+    // few rows, or short ones: as many warps as a row feeds; else more bytes in flight a lane
     Shape s{0, 0, 0};
-    for (int nv = a.rows <= n_sm ? 1 : SHIFT ? 2 : 4; nv <= 4 && s.nv == 0; nv *= 2) s = row_shape(a.cols, SHIFT, nv, quantize_warps(nv));
+    for (int nv = a.rows <= n_sm || a.cols <= 256 ? 1 : a.cols <= 512 ? 2 : 4; nv <= 4 && s.nv == 0; nv *= 2) s = row_shape(a.cols, nv, quantize_warps(nv));
+    if (s.nv == 0) s.warps = quantize_warps(0);
     const dim3 block(32 * s.warps, s.teams);
     const unsigned grid = (unsigned)((a.rows + s.teams - 1) / s.teams);
-    if (s.nv == 0) k_rows_quantize<OP, DT, SHIFT, 0><<<grid, block, 0, st>>>(a);
-    else if (s.nv == 1) k_rows_quantize<OP, DT, SHIFT, 1><<<grid, block, 0, st>>>(a);
-    else if (s.nv == 2) k_rows_quantize<OP, DT, SHIFT, 2><<<grid, block, 0, st>>>(a);
-    else k_rows_quantize<OP, DT, SHIFT, 4><<<grid, block, 0, st>>>(a);
+    if (s.nv == 0) k_rows_quantize<OP, DT, VEC, 0><<<grid, block, 0, st>>>(a);
+    else if (s.nv == 1) k_rows_quantize<OP, DT, VEC, 1><<<grid, block, 0, st>>>(a);
+    else if (s.nv == 2) k_rows_quantize<OP, DT, VEC, 2><<<grid, block, 0, st>>>(a);
+    else k_rows_quantize<OP, DT, VEC, 4><<<grid, block, 0, st>>>(a);
 }
 
 // ---- gradients -------------------------------------------------------------------------------------------------
+// fp32 values from one team's slice of partial sums to the next: slices start on 16 bytes
+__host__ __device__ inline int64_t slice_stride(int64_t cols) { return (cols + 3) / 4 * 4; }
+
 struct NormBackArgs {
     const void *dy, *h, *dh;  // dh nullable
     const float* weight;      // nullable
     void* dx;
-    float* part;              // [teams of the grid][cols] partial sums of dweight (nullable)
+    float* part;              // [blocks][slice_stride(cols)] partial sums of dweight (nullable)
     int64_t lddy, ldh, lddh, lddx, rows, cols;
     float eps;
 };
 
-// A team takes rows in steps of the number of teams.  A lane keeps its columns, so the weights and the partial sums of
-// dweight have a fixed place in shared memory (registers are what limits the rows in flight), NV pieces of two 16-byte
-// vectors a lane; with NV = 0 the sums are in the team's slice of the workspace all along.
-template <int DT, bool SHIFT, int NV>
-__global__ void __launch_bounds__(32 * backward_warps(NV), NV == 1 ? 2 : 1) k_norm_backward(const NormBackArgs a) {
-    typedef typename Store<DT>::type T;
-    extern __shared__ float4 s_cols[];  // weights, then sums: [NV][2][threads of the block] each
-    __shared__ uint32_t s_scratch[kBlockWarps][2][96];
-    const Team team{(int)(blockDim.x >> 5), (int)(threadIdx.x >> 5), (int)threadIdx.y};
-    const Lanes<SHIFT> at{team.warps, team.warp, (int)(threadIdx.x & 31)};
-    const int cols = (int)a.cols;
-    constexpr int kHeld = NV ? NV : 1;
-    const int threads = blockDim.x * blockDim.y, self = threadIdx.y * blockDim.x + threadIdx.x;
-    const int64_t me = (int64_t)blockIdx.x * blockDim.y + threadIdx.y, teams = (int64_t)gridDim.x * blockDim.y;
-    if (me >= a.rows) return;  // (a whole team; it has no slice of the workspace)
-    float* part = a.part ? a.part + me * a.cols : nullptr;
-    const float inv_n = 1.0f / (float)cols;
-    auto weights = [&](int c, float (&p)[8]) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = 1.0f;
-        if (a.weight) load8<SHIFT>(a.weight, c, cols, p);
-    };
-    auto kept = [&](int which, int j, float (&p)[8]) {
-        const float4 x = s_cols[((which * kHeld + j) * 2) * threads + self], y = s_cols[((which * kHeld + j) * 2 + 1) * threads + self];
-        p[0] = x.x, p[1] = x.y, p[2] = x.z, p[3] = x.w, p[4] = y.x, p[5] = y.y, p[6] = y.z, p[7] = y.w;
-    };
-    auto keep = [&](int which, int j, const float (&p)[8]) {
-        s_cols[((which * kHeld + j) * 2) * threads + self] = make_float4(p[0], p[1], p[2], p[3]);
-        s_cols[((which * kHeld + j) * 2 + 1) * threads + self] = make_float4(p[4], p[5], p[6], p[7]);
-    };
-    auto give_part = [&](int c, const float (&p)[8]) {
-        if (!at.counted()) return;
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (c + e >= 0 && c + e < cols) part[c + e] = p[e];
-    };
-    if constexpr (NV != 0) {
-#pragma unroll
-        for (int j = 0; j < kHeld; ++j) {
-            float p[8];
-            weights(at.column(j), p);
-            keep(0, j, p);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) p[e] = 0.0f;
-            keep(1, j, p);
-        }
+// A row in a stage of shared memory.  Its bytes keep their place within 16, so that it can be copied in whole 16-byte pieces:
+// the first may begin before the row (still in the row's allocation, which starts on 16 bytes), the last is cut at its end.
+template <typename T>
+__device__ __forceinline__ int row_shift(const T* row) { return (int)((reinterpret_cast<uintptr_t>(row) / sizeof(T)) & (16 / sizeof(T) - 1)); }
+
+// Copies 16 bytes, or the `bytes` that are left of a row and zeros behind them; nothing where none is left.
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, int bytes) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.gt.s32 p, %2, 0;\n\t@p cp.async.cg.shared.global [%0], [%1], 16, %3;\n\t}" ::"r"(to), "l"(from), "r"(bytes),
+                 "r"(min(16, bytes))
+                 : "memory");
+}
+// One matrix on its way into the stages: this thread's pieces.  VEC: those of its own columns, so that no other thread waits for
+// them; else every blockDim.x-th piece of the row's span, which is up to one longer than the team has places for.
+template <bool VEC, int NV, typename T>
+struct Copier {
+    static constexpr int kEach = NV * (int)sizeof(T) / 2;
+    const char* row;  // of the next copy; VEC: from this thread's first column on
+    int64_t step;     // bytes from row to row
+    __device__ __forceinline__ void init(const void* m, int64_t ld, int64_t r, int64_t teams) {
+        row = static_cast<const char*>(m) + (r * ld + (VEC ? 8 * (int)threadIdx.x : 0)) * (int64_t)sizeof(T);
+        step = teams * ld * (int64_t)sizeof(T);
     }
-    int side = 0;
-    for (int64_t r = me; r < a.rows; r += teams, side ^= 1) {
-        const T* dy = static_cast<const T*>(a.dy) + r * a.lddy;
-        const T* h = static_cast<const T*>(a.h) + r * a.ldh;
-        const T* dh = static_cast<const T*>(a.dh) + r * a.lddh;
-        T* dx = static_cast<T*>(a.dx) + r * a.lddx;
-        float hv[kHeld][8], gv[kHeld][8], pv[kHeld][8], w[8], sum[8];
-        float sq = 0.0f, along = 0.0f;
-        uint32_t unused = 0;
-        auto fetch = [&](int c, Piece<SHIFT, T> (&p)[3]) {
-            p[0].fetch(h, c, cols);
-            p[1].fetch(dy, c, cols);
-            if (a.dh) p[2].fetch(dh, c, cols);
-        };
-        auto get = [&](int c, const Piece<SHIFT, T> (&p)[3], float (&hp)[8], float (&gp)[8], float (&pp)[8]) {
-            p[0].get(h, c, cols, hp);
-            p[1].get(dy, c, cols, gp);
+    __device__ __forceinline__ void next(uint32_t stage, int cols) {
+        const int t = threadIdx.x, threads = blockDim.x;
+        if constexpr (VEC) {
+            constexpr int kSpan = 8 * sizeof(T);
+            const uint32_t to = stage + t * kSpan;
+            const int left = (cols - 8 * t) * (int)sizeof(T);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) pp[e] = 0.0f;
-            if (a.dh) p[2].get(dh, c, cols, pp);
-        };
-        auto sums = [&](const float (&hp)[8], const float (&gp)[8]) {
-            if (!at.counted()) return;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sq = fmaf(hp[e], hp[e], sq), along = fmaf(gp[e] * w[e], hp[e], along);
-        };
-        if constexpr (NV != 0) {
-            Piece<SHIFT, T> p[kHeld][3];
-#pragma unroll
-            for (int j = 0; j < kHeld; ++j) fetch(at.column(j), p[j]);
-#pragma unroll
-            for (int j = 0; j < kHeld; ++j) {
-                get(at.column(j), p[j], hv[j], gv[j], pv[j]);
-                kept(0, j, w);
-                sums(hv[j], gv[j]);
+            for (int j = 0; j < kEach; ++j) {
+                const int at = j / (kSpan / 16) * threads * kSpan + j % (kSpan / 16) * 16;
+                copy16(to + at, row + at, left - at);
             }
         } else {
-            for (int j = 0; j * team.warps * at.kPieces < row_pieces<SHIFT>(cols); ++j) {
-                load8<SHIFT>(h, at.column(j), cols, hv[0]);
-                load8<SHIFT>(dy, at.column(j), cols, gv[0]);
-                weights(at.column(j), w);
-                sums(hv[0], gv[0]);
-            }
+            const int lead = (int)(reinterpret_cast<uintptr_t>(row) & 15), bytes = lead + cols * (int)sizeof(T);
+            const char* from = row - lead + 16 * t;
+            const uint32_t to = stage + 16 * t;
+#pragma unroll
+            for (int j = 0; j < kEach; ++j)
+                copy16(to + 16 * j * threads, from + 16 * j * threads, bytes - 16 * (t + j * threads));
+            const int more = kEach * threads * 16;
+            if (t == 0) copy16(to + more, from + more, bytes - more);
         }
-        // (two buffers: the barrier of a row frees the buffer of the row before.  It also orders every fetch of the row before
-        // the first store to it, where dx is one of the inputs.)
-        team_reduce<true, true, false>(team, sq, along, unused, s_scratch[team.id][side]);
-        const float root = 1.0f / sqrtf(sq * inv_n + a.eps);
-        const float coef = along * root * inv_n;
-        auto give = [&](int c, const float (&hp)[8], const float (&gp)[8], const float (&pp)[8]) {
-            float o[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float unit = hp[e] * root;
-                o[e] = fmaf(root, fmaf(gp[e], w[e], -unit * coef), pp[e]);
-                sum[e] = fmaf(gp[e], unit, sum[e]);
-            }
-            store8<SHIFT>(dx, c, cols, o);
-        };
-        if constexpr (NV != 0) {
-#pragma unroll
-            for (int j = 0; j < kHeld; ++j) {
-                kept(0, j, w);
-                kept(1, j, sum);
-                give(at.column(j), hv[j], gv[j], pv[j]);
-                keep(1, j, sum);
-            }
-        } else {
-            float hn[8], gn[8], pn[8];
-            Piece<SHIFT, T> p[3];
-            fetch(at.column(0), p);
-            get(at.column(0), p, hv[0], gv[0], pv[0]);
-            for (int j = 0; j * team.warps * at.kPieces < row_pieces<SHIFT>(cols); ++j) {
-                const int c = at.column(j);
-                if ((j + 1) * team.warps * at.kPieces < row_pieces<SHIFT>(cols)) {
-                    fetch(at.column(j + 1), p);
-                    get(at.column(j + 1), p, hn, gn, pn);
-                }
-                if (SHIFT) team.sync();  // (as in the second walk of k_rows_quantize)
-                weights(c, w);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sum[e] = part && r != me && c + e >= 0 && c + e < cols ? part[c + e] : 0.0f;
-                give(c, hv[0], gv[0], pv[0]);
-                if (part) give_part(c, sum);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) hv[0][e] = hn[e], gv[0][e] = gn[e], pv[0][e] = pn[e];
-            }
-        }
+        row += step;
     }
-    if constexpr (NV != 0) {
-        if (part) {
+};
+
+// A lane's columns c, c + step, ... of a staged row; those past its end as 0.
+template <bool VEC, typename T>
+__device__ __forceinline__ void staged8(const T* row, const unsigned char* stage, int c, int cols, float (&v)[8]) {
+    const T* p = reinterpret_cast<const T*>(stage) + (VEC ? 0 : row_shift(row)) + c;
+    if constexpr (VEC && sizeof(T) == 2) {
+        uint4 a = make_uint4(0, 0, 0, 0);
+        if (c < cols) a = *reinterpret_cast<const uint4*>(p);  // (past the end the copy left zeros)
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-            for (int j = 0; j < kHeld; ++j) {
-                float p[8];
-                kept(1, j, p);
-                give_part(at.column(j), p);
-            }
+        for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
+    } else if constexpr (VEC) {
+        float4 a = make_float4(0, 0, 0, 0), b = a;
+        if (c < cols) a = *reinterpret_cast<const float4*>(p);
+        if (c + 4 < cols) b = *reinterpret_cast<const float4*>(p + 4);
+        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    } else {
+        T x[8];
+        if (piece_inside<false>(c, cols)) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = p[32 * e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = c + 32 * e < cols ? p[32 * e] : T(0);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if constexpr (sizeof(T) == 4) v[e] = x[e];
+            else v[e] = __uint_as_float((uint32_t)x[e] << 16);
         }
     }
 }
 
-// dweight[c] = sum of the teams' partial sums in a fixed order: 32 columns by 32 runs of teams a block.
-__global__ void __launch_bounds__(1024) k_norm_weight_sum(const float* __restrict__ part, int64_t teams, int64_t cols, float* __restrict__ dweight) {
-    __shared__ float s[32][33];
-    const int64_t c = (int64_t)blockIdx.x * 32 + threadIdx.x;
-    float sum = 0.0f;
-    if (c < cols) {
-#pragma unroll 4
-        for (int64_t g = threadIdx.y; g < teams; g += 32) sum += part[g * cols + c];
-    }
-    s[threadIdx.y][threadIdx.x] = sum;
-    __syncthreads();
-    // warp y adds up column y of the block's 32
-    float all = s[threadIdx.x][threadIdx.y];
+// A team takes rows in steps of the number of teams.  Its rows pass through `stages` stages of shared memory that asynchronous
+// copies fill ahead, so that what is in flight does not depend on where the team stands between its barriers.  A lane keeps its
+// columns, so the weights and the partial sums of dweight stay in registers, NV pieces of 8.  blockDim: (32 * warps, teams), more
+// than one team only of one warp.
+template <int DT, bool VEC, int NV>
+__global__ void __launch_bounds__(32 * backward_warps(NV), NV == 4 ? 1 : 2) k_norm_backward(const NormBackArgs a, int stages, uint32_t row_bytes) {
+    typedef typename Store<DT>::type T;
+    extern __shared__ __align__(16) unsigned char s_rows[];  // [teams of the block][stages][3][row_bytes]
+    __shared__ __align__(16) float2 s_scratch[2][16];
+    const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5;
+    const int cols = (int)a.cols;
+    const int64_t me = (int64_t)blockIdx.x * blockDim.y + threadIdx.y, teams = (int64_t)gridDim.x * blockDim.y;
+    const float inv_n = 1.0f / (float)cols;
+    constexpr bool kHold = NV == 1;  // a row's values stay in registers over the reduction (NV > 1: they would spill)
+    auto column = [&](int j) { return first_column<VEC>(j, warps, warp); };
+    const uint32_t stage_bytes = 3 * row_bytes;
+    unsigned char* const first = s_rows + threadIdx.y * stages * stage_bytes;
+    unsigned char* const last = first + (stages - 1) * stage_bytes;
+    Copier<VEC, NV, T> copy_h, copy_dy, copy_dh;
+    copy_h.init(a.h, a.ldh, me, teams);
+    copy_dy.init(a.dy, a.lddy, me, teams);
+    copy_dh.init(a.dh, a.lddh, me, teams);
+    auto copy = [&](unsigned char* stage, bool there) {
+        const uint32_t to = (uint32_t)__cvta_generic_to_shared(stage);
+        if (there) {
+            copy_h.next(to, cols);
+            copy_dy.next(to + row_bytes, cols);
+            if (a.dh) copy_dh.next(to + 2 * row_bytes, cols);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    for (int s = 0; s < stages - 1; ++s) copy(first + s * stage_bytes, me + s * teams < a.rows);
+    float w[NV][8], sum[NV][8];
 #pragma unroll
-    for (int d = 16; d; d >>= 1) all += __shfl_xor_sync(kFullMask, all, d);
-    const int64_t out = (int64_t)blockIdx.x * 32 + threadIdx.y;
-    if (threadIdx.x == 0 && out < cols) dweight[out] = all;
+    for (int j = 0; j < NV; ++j) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[j][e] = 1.0f, sum[j][e] = 0.0f;
+        if (a.weight) load8<VEC>(a.weight, column(j), cols, w[j]);
+    }
+    // where rows start within 16 bytes (all of them the same in VEC: 0)
+    const T* h = static_cast<const T*>(a.h) + me * a.ldh;
+    const T* dy = static_cast<const T*>(a.dy) + me * a.lddy;
+    const T* dh = static_cast<const T*>(a.dh) + me * a.lddh;
+    T* dx = static_cast<T*>(a.dx) + me * a.lddx;
+    const int64_t step_h = teams * a.ldh, step_dy = teams * a.lddy, step_dh = teams * a.lddh, step_dx = teams * a.lddx;
+    int side = 0;
+    unsigned char* stage = first;
+    for (int64_t r = me, ahead = me + (stages - 1) * teams; r < a.rows; r += teams, ahead += teams, side ^= 1) {
+        // the row is there: this thread's copies and, past the barrier, everybody's; past it the stage before is free, too.  (VEC: a
+        // thread reads what it copied itself, and needs neither.)
+        if (stages == 2) asm volatile("cp.async.wait_group 0;" ::: "memory");
+        else if (stages == 3) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        else asm volatile("cp.async.wait_group 2;" ::: "memory");
+        if constexpr (!VEC) {
+            if (warps == 1) __syncwarp();
+            else __syncthreads();
+        }
+        copy(stage == first ? last : stage - stage_bytes, ahead < a.rows);
+        float hv[kHold ? NV : 1][8], gv[kHold ? NV : 1][8], sq = 0.0f, along = 0.0f;
+        auto get = [&](int j) {
+            staged8<VEC>(h, stage, column(j), cols, hv[kHold ? j : 0]);
+            staged8<VEC>(dy, stage + row_bytes, column(j), cols, gv[kHold ? j : 0]);
+        };
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            get(j);
+            const int i = kHold ? j : 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sq = fmaf(hv[i][e], hv[i][e], sq), along = fmaf(gv[i][e] * w[j][e], hv[i][e], along);
+        }
+        // (two buffers: the barrier of a row frees the buffer of the row before)
+        reduce_two_sums(warps, sq, along, s_scratch[side]);
+        const float root = rsqrtf(sq * inv_n + a.eps);
+        const float coef = along * root * inv_n * root;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int i = kHold ? j : 0;
+            float o[8];
+            if (!kHold) get(j);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = 0.0f;
+            if (a.dh) staged8<VEC>(dh, stage + 2 * row_bytes, column(j), cols, o);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float g = gv[i][e] * root;
+                o[e] = fmaf(g, w[j][e], fmaf(-coef * root, hv[i][e], o[e]));
+                sum[j][e] = fmaf(g, hv[i][e], sum[j][e]);
+            }
+            store8<VEC>(dx, column(j), cols, o);
+        }
+        dx += step_dx;
+        if constexpr (!VEC) h += step_h, dy += step_dy, dh += step_dh;
+        stage = stage == last ? first : stage + stage_bytes;
+    }
+    if (!a.part) return;
+    if constexpr (NV == 1) {
+        // teams of one warp: the block's are added up here
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncthreads();
+        float* all = reinterpret_cast<float*>(s_rows) + threadIdx.y * 256;
+        const int lane = threadIdx.x;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) all[(VEC ? 8 * lane : lane) + kStep<VEC> * e] = sum[0][e];
+        __syncthreads();
+        const int c = threadIdx.y * 32 + lane;
+        float total = 0.0f;
+        for (int i = 0; i < (int)blockDim.y; ++i) total += reinterpret_cast<const float*>(s_rows)[i * 256 + c];
+        if (c < cols) a.part[blockIdx.x * slice_stride(a.cols) + c] = total;
+    } else {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) store8<VEC>(a.part + me * slice_stride(a.cols), column(j), cols, sum[j]);
+    }
+}
+
+// The same for rows that do not fit in shared memory: walked twice, the partial sums in the team's slice of the workspace.
+template <int DT, bool VEC>
+__global__ void __launch_bounds__(512) k_norm_backward_long(const NormBackArgs a) {
+    typedef typename Store<DT>::type T;
+    __shared__ __align__(16) float2 s_scratch[2][16];
+    const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5;
+    const int cols = (int)a.cols;
+    float* part = a.part ? a.part + blockIdx.x * slice_stride(a.cols) : nullptr;
+    const float inv_n = 1.0f / (float)cols;
+    auto column = [&](int j) { return first_column<VEC>(j, warps, warp); };
+    int side = 0;
+    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x, side ^= 1) {
+        const T* hr = static_cast<const T*>(a.h) + r * a.ldh;
+        const T* dyr = static_cast<const T*>(a.dy) + r * a.lddy;
+        float sq = 0.0f, along = 0.0f, w[8];
+        Raw<VEC, T> h, dy, dh;
+        auto weights = [&](int c) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = 1.0f;
+            if (a.weight) load8<VEC>(a.weight, c, cols, w);
+        };
+        for (int j = 0; column(j) < cols; ++j) {
+            h.fetch(hr, column(j), cols);
+            dy.fetch(dyr, column(j), cols);
+            weights(column(j));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sq = fmaf(h.get(e), h.get(e), sq), along = fmaf(dy.get(e) * w[e], h.get(e), along);
+        }
+        __syncwarp();
+        reduce_two_sums(warps, sq, along, s_scratch[side]);
+        const float root = rsqrtf(sq * inv_n + a.eps);
+        const float coef = along * root * inv_n;
+        for (int j = 0; column(j) < cols; ++j) {
+            const int c = column(j);
+            float o[8], sum[8];
+            h.fetch(hr, c, cols);
+            dy.fetch(dyr, c, cols);
+            if (a.dh) dh.fetch(static_cast<const T*>(a.dh) + r * a.lddh, c, cols);
+            weights(c);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
+            if (part && r != blockIdx.x) load8<VEC>(part, c, cols, sum);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float unit = h.get(e) * root, g = dy.get(e);
+                o[e] = fmaf(root, fmaf(g, w[e], -unit * coef), a.dh ? dh.get(e) : 0.0f);
+                sum[e] = fmaf(g, unit, sum[e]);
+            }
+            store8<VEC>(static_cast<T*>(a.dx) + r * a.lddx, c, cols, o);
+            if (part) store8<VEC>(part, c, cols, sum);
+        }
+    }
+}
+
+// dweight[c] = sum of the teams' partial sums in a fixed order: 8 columns (a sector) by 32 runs of teams a block.
+__global__ void __launch_bounds__(256) k_norm_weight_sum(const float* __restrict__ part, int64_t teams, int64_t cols, float* __restrict__ dweight) {
+    __shared__ float s[32][9];
+    const int64_t c0 = (int64_t)blockIdx.x * 8;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = threadIdx.x & 7, run = threadIdx.x >> 3;
+    float sum = 0.0f;
+    if (c0 + col < cols) {
+#pragma unroll 8
+        for (int64_t g = run; g < teams; g += 32) sum += part[g * slice_stride(cols) + c0 + col];
+    }
+    s[run][col] = sum;
+    __syncthreads();
+    if (c0 + warp < cols) {
+        float all = s[lane][warp];
+#pragma unroll
+        for (int d = 16; d; d >>= 1) all += __shfl_xor_sync(kFullMask, all, d);
+        if (lane == 0) dweight[c0 + warp] = all;
+    }
 }
 
 struct GateBackArgs {
@@ -617,52 +687,28 @@ struct GateBackArgs {
     int64_t lddy, ldg, ldu, lddg, lddu, rows, cols;
 };
 
-// A team works on rounds of one piece a lane: all rounds of a row (ALIAS: an output is an input, and rows do not start on 16
-// bytes, so the team fetches a round and the next before it stores the first), or those of its share of the grid.
-template <int DT, bool SHIFT, bool ALIAS>
+// blockIdx.x: rows, by teams of a block; blockIdx.y: pieces of a row, by warps of a team.
+template <int DT, bool VEC>
 __global__ void __launch_bounds__(32 * kBlockWarps) k_gate_backward(const GateBackArgs a) {
     typedef typename Store<DT>::type T;
-    const Team team{(int)(blockDim.x >> 5), (int)(threadIdx.x >> 5), (int)threadIdx.y};
-    const Lanes<SHIFT> at{team.warps, team.warp, (int)(threadIdx.x & 31)};
-    const int cols = (int)a.cols;
-    const int rounds = (row_pieces<SHIFT>(cols) + team.warps * at.kPieces - 1) / (team.warps * at.kPieces);
+    const int cols = (int)a.cols, warps = blockDim.x >> 5, warp = threadIdx.x >> 5;
     for (int64_t r = (int64_t)blockIdx.x * blockDim.y + threadIdx.y; r < a.rows; r += (int64_t)gridDim.x * blockDim.y) {
-        const T* dy = static_cast<const T*>(a.dy) + r * a.lddy;
-        const T* gate = static_cast<const T*>(a.gate) + r * a.ldg;
-        const T* up = static_cast<const T*>(a.up) + r * a.ldu;
-        T* dgate = static_cast<T*>(a.dgate) + r * a.lddg;
-        T* dup = static_cast<T*>(a.dup) + r * a.lddu;
-        float d[8], g[8], u[8], dn[8], gn[8], un[8];
-        auto fetch = [&](int c, float (&dp)[8], float (&gp)[8], float (&up8)[8]) {
-            Piece<SHIFT, T> p, q, o;
-            p.fetch(dy, c, cols);
-            q.fetch(gate, c, cols);
-            o.fetch(up, c, cols);
-            p.get(dy, c, cols, dp);
-            q.get(gate, c, cols, gp);
-            o.get(up, c, cols, up8);
-        };
-        if (ALIAS) fetch(at.column(0), d, g, u);
-        for (int j = blockIdx.y; j < rounds; j += gridDim.y) {
-            const int c = at.column(j);
-            if (ALIAS) {
-                if (j + 1 < rounds) fetch(at.column(j + 1), dn, gn, un);
-                team.sync();
-            } else {
-                fetch(c, d, g, u);
-            }
+        for (int j = blockIdx.y;; j += gridDim.y) {
+            const int c = first_column<VEC>(j, warps, warp);
+            if ((j * warps + warp) * 256 >= cols) break;
+            Raw<VEC, T> d, g, u;
+            d.fetch(static_cast<const T*>(a.dy) + r * a.lddy, c, cols);
+            g.fetch(static_cast<const T*>(a.gate) + r * a.ldg, c, cols);
+            u.fetch(static_cast<const T*>(a.up) + r * a.ldu, c, cols);
+            float dg[8], du[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float s = sigmoid(g[e]), ds = d[e] * s;
-                u[e] = ds * u[e] * fmaf(g[e], 1.0f - s, 1.0f);
-                d[e] = ds * g[e];
+                const float x = g.get(e), s = sigmoid(x), ds = d.get(e) * s;
+                dg[e] = ds * u.get(e) * fmaf(x, 1.0f - s, 1.0f);
+                du[e] = ds * x;
             }
-            store8<SHIFT>(dgate, c, cols, u);
-            store8<SHIFT>(dup, c, cols, d);
-            if (ALIAS) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) d[e] = dn[e], g[e] = gn[e], u[e] = un[e];
-            }
+            store8<VEC>(static_cast<T*>(a.dgate) + r * a.lddg, c, cols, dg);
+            store8<VEC>(static_cast<T*>(a.dup) + r * a.lddu, c, cols, du);
         }
     }
 }
@@ -719,52 +765,57 @@ dnns_status run_quantize(const QuantArgs& a, int32_t dtype, void* stream) {
     const size_t e = elem_bytes(dtype);
     const bool vec = on_16(a.x, a.ldx, a.rows, e) && (!a.x2 || on_16(a.x2, a.ldx2, a.rows, e)) && (!a.h || on_16(a.h, a.ldh, a.rows, e)) &&
                      (!a.values || on_16(a.values, a.ldv, a.rows, 2)) && (!a.weight || on_16(a.weight, 0, 1, 4));
-    if (dtype == DNNS_F32) vec ? launch_quantize<OP, DNNS_F32, false>(a, n_sm, st) : launch_quantize<OP, DNNS_F32, true>(a, n_sm, st);
-    else vec ? launch_quantize<OP, DNNS_BF16, false>(a, n_sm, st) : launch_quantize<OP, DNNS_BF16, true>(a, n_sm, st);
+    if (dtype == DNNS_F32) vec ? launch_quantize<OP, DNNS_F32, true>(a, n_sm, st) : launch_quantize<OP, DNNS_F32, false>(a, n_sm, st);
+    else vec ? launch_quantize<OP, DNNS_BF16, true>(a, n_sm, st) : launch_quantize<OP, DNNS_BF16, false>(a, n_sm, st);
     return cudaGetLastError() == cudaSuccess ? DNNS_OK : DNNS_ERR_CUDA;
 }
 
-// Teams of the norm's gradient: as many as stay busy on the 148 SMs with at least 16 rows each, so that the partial sums of
-// dweight, one row of fp32 a team, stay small beside the matrices.
-Shape norm_backward_shape(int64_t cols, bool shift) {
-    Shape s{0, 0, 0};
-    for (int nv = 1; nv <= 2 && s.nv == 0; nv *= 2) s = row_shape(cols, shift, nv, backward_warps(nv));
-    if (s.nv == 0) s.warps = backward_warps(0);
+// Warps of a team of the norm's gradient: NV = 2 up to 4096 columns, 4 above (fewer warps, but the weights and sums of 8 more
+// columns a lane in registers); 16 warps where 8 do not hold a row.
+Shape norm_backward_shape(int64_t cols) {
+    if (cols <= 256) return row_shape(cols, 1, 1);
+    Shape s = row_shape(cols, cols <= 512 * backward_warps(2) ? 2 : 4, 16);
+    s.teams = 1;
     return s;
 }
-int64_t norm_backward_teams(int64_t rows, int64_t cols) {
-    const Shape s = norm_backward_shape(cols, true);
-    const int64_t room = 148 * std::max(1, (s.nv == 1 ? 32 : 20) / s.warps);  // (64 and 96 registers a thread)
-    return std::min(rows, std::min(room, std::max<int64_t>(148, rows / 16)));
+// Blocks of an SM at most: about 16 warps of about 112 registers a thread; the workspace is sized for that many, a slice a block.
+int norm_backward_blocks(const Shape& s) { return std::max(1, 18 / (s.warps * s.teams)); }
+int64_t norm_backward_slices(int64_t rows, int64_t cols) {
+    const Shape s = norm_backward_shape(cols);
+    return std::min<int64_t>((rows + s.teams - 1) / s.teams, 148 * norm_backward_blocks(s));
 }
 
-template <int DT, bool SHIFT>
-bool launch_norm_backward(const NormBackArgs& a, cudaStream_t st) {
-    static std::atomic<uint64_t> done{0};
-    Shape s = norm_backward_shape(a.cols, SHIFT);
-    const int64_t teams = norm_backward_teams(a.rows, a.cols);
-    while (teams % s.teams) --s.teams;  // (every team of the grid has a slice of the workspace)
-    const unsigned grid = (unsigned)(teams / s.teams);
-    const dim3 block(32 * s.warps, s.teams);
-    const size_t shared = (size_t)s.nv * 2 * 32 * block.x * block.y;
-    if (s.nv == 0) k_norm_backward<DT, SHIFT, 0><<<grid, block, 0, st>>>(a);
-    else if (s.nv == 1) k_norm_backward<DT, SHIFT, 1><<<grid, block, shared, st>>>(a);
-    else {
-        int dev = 0;
-        if (cudaGetDevice(&dev) != cudaSuccess || !allow_shared(k_norm_backward<DT, SHIFT, 2>, 2 * 2 * 32 * 32 * backward_warps(2), done, dev)) return false;
-        k_norm_backward<DT, SHIFT, 2><<<grid, block, shared, st>>>(a);
+// Launches the gradient; how many slices of partial sums it writes, or -1.
+template <int DT, bool VEC>
+int64_t launch_norm_backward(const NormBackArgs& a, cudaStream_t st) {
+    static std::atomic<uint64_t> done[3];
+    constexpr size_t kRoom = 200 * 1024;  // shared memory of an SM that the stages may take
+    const Shape s = norm_backward_shape(a.cols);
+    const size_t row_bytes = ((size_t)a.cols * (DT == DNNS_F32 ? 4 : 2) + 15) / 16 * 16 + (VEC ? 0 : 16), stage = 3 * row_bytes * s.teams;
+    int blocks = norm_backward_blocks(s);
+    while (blocks > 1 && kRoom / blocks < 3 * stage) --blocks;
+    const int stages = (int)std::min<size_t>(4, kRoom / blocks / stage);
+    if (s.nv == 0 || stages < 2) {
+        const int64_t grid = std::min<int64_t>(a.rows, 148);
+        k_norm_backward_long<DT, VEC><<<(unsigned)grid, 512, 0, st>>>(a);
+        return grid;
     }
-    return true;
+    const int64_t grid = std::min<int64_t>((a.rows + s.teams - 1) / s.teams, 148 * blocks);
+    const dim3 block(32 * s.warps, s.teams);
+    const auto kernel = s.nv == 1 ? k_norm_backward<DT, VEC, 1> : s.nv == 2 ? k_norm_backward<DT, VEC, 2> : k_norm_backward<DT, VEC, 4>;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || !allow_shared(kernel, kRoom, done[s.nv / 2], dev)) return -1;
+    const size_t shared = std::max(stages * stage, s.nv == 1 ? (size_t)kBlockWarps * 256 * sizeof(float) : 0);
+    kernel<<<(unsigned)grid, block, shared, st>>>(a, stages, (uint32_t)row_bytes);
+    return grid;
 }
 
-template <int DT, bool SHIFT, bool ALIAS>
-void launch_gate_backward(const GateBackArgs& a, int n_sm, cudaStream_t st) {
-    Shape s = row_shape(a.cols, SHIFT, 1, kBlockWarps);
-    if (s.nv == 0) s = Shape{1, kBlockWarps, 1};
-    const int lanes = SHIFT ? 31 : 32;
-    const int rounds = (row_pieces<SHIFT>((int)a.cols) + lanes * s.warps - 1) / (lanes * s.warps);
-    const dim3 grid((unsigned)std::min<int64_t>((a.rows + s.teams - 1) / s.teams, (int64_t)1 << 30), ALIAS ? 1 : std::min(rounds, 65535));
-    k_gate_backward<DT, SHIFT, ALIAS><<<grid, dim3(32 * s.warps, s.teams), 0, st>>>(a);
+template <int DT, bool VEC>
+void launch_gate_backward(const GateBackArgs& a, cudaStream_t st) {
+    Shape s = row_shape(a.cols, 1, kBlockWarps);
+    const int rounds = (int)((a.cols + 256 * s.warps - 1) / (256 * s.warps));
+    const dim3 grid((unsigned)std::min<int64_t>((a.rows + s.teams - 1) / s.teams, (int64_t)1 << 30), std::min(rounds, 65535));
+    k_gate_backward<DT, VEC><<<grid, dim3(32 * s.warps, s.teams), 0, st>>>(a);
 }
 
 bool eps_ok(float eps) { return eps >= 0x1p-126f && eps <= 3.402823466e38f; }
@@ -800,7 +851,7 @@ dnns_status dnns_silu_gate_quantize(const void* gate, int64_t ldg, const void* u
 
 size_t dnns_rmsnorm_backward_workspace_bytes(int64_t rows, int64_t cols) {
     if (rows <= 0 || cols <= 0 || !dnns::extent_ok(rows, cols)) return 0;
-    return ((size_t)dnns::norm_backward_teams(rows, cols) * (size_t)cols * sizeof(float) + 255) & ~(size_t)255;
+    return ((size_t)dnns::norm_backward_slices(rows, cols) * (size_t)dnns::slice_stride(cols) * sizeof(float) + 255) & ~(size_t)255;
 }
 
 dnns_status dnns_rmsnorm_backward(const void* dy, int64_t lddy, const void* h, int64_t ldh, const float* weight, float eps,
@@ -828,10 +879,10 @@ dnns_status dnns_rmsnorm_backward(const void* dy, int64_t lddy, const void* h, i
     const NormBackArgs a{dy, h, dh, weight, dx, dweight ? static_cast<float*>(ws_dev) : nullptr, lddy, ldh, lddh, lddx, rows, cols, eps};
     const bool vec = on_16(dy, lddy, rows, e) && on_16(h, ldh, rows, e) && on_16(dx, lddx, rows, e) && (!dh || on_16(dh, lddh, rows, e)) &&
                      (!weight || on_16(weight, 0, 1, 4));
-    const bool launched = dtype == DNNS_F32 ? (vec ? launch_norm_backward<DNNS_F32, false>(a, st) : launch_norm_backward<DNNS_F32, true>(a, st))
-                                            : (vec ? launch_norm_backward<DNNS_BF16, false>(a, st) : launch_norm_backward<DNNS_BF16, true>(a, st));
-    if (!launched) return DNNS_ERR_CUDA;
-    if (dweight) k_norm_weight_sum<<<(unsigned)((cols + 31) / 32), dim3(32, 32), 0, st>>>(a.part, norm_backward_teams(rows, cols), cols, dweight);
+    const int64_t slices = dtype == DNNS_F32 ? (vec ? launch_norm_backward<DNNS_F32, true>(a, st) : launch_norm_backward<DNNS_F32, false>(a, st))
+                                            : (vec ? launch_norm_backward<DNNS_BF16, true>(a, st) : launch_norm_backward<DNNS_BF16, false>(a, st));
+    if (slices < 0) return DNNS_ERR_CUDA;
+    if (dweight) k_norm_weight_sum<<<(unsigned)((cols + 7) / 8), 256, 0, st>>>(a.part, slices, cols, dweight);
     return cudaGetLastError() == cudaSuccess ? DNNS_OK : DNNS_ERR_CUDA;
 }
 
@@ -848,17 +899,12 @@ dnns_status dnns_silu_gate_backward(const void* dy, int64_t lddy, const void* ga
         return DNNS_ERR_INVALID_ARG;
     if (!span_ok(rows, lddy) || !span_ok(rows, ldg) || !span_ok(rows, ldu) || !span_ok(rows, lddg) || !span_ok(rows, lddu))
         return DNNS_ERR_UNSUPPORTED;
-    const int n_sm = sm_count();
-    if (n_sm == 0) return DNNS_ERR_CUDA;
     const GateBackArgs a{dy, gate, up, dgate, dup, lddy, ldg, ldu, lddg, lddu, rows, cols};
     const bool vec = on_16(dy, lddy, rows, e) && on_16(gate, ldg, rows, e) && on_16(up, ldu, rows, e) && on_16(dgate, lddg, rows, e) &&
                      on_16(dup, lddu, rows, e);
-    bool alias = false;
-    for (const void* out : {dgate, dup}) alias = alias || out == dy || out == gate || out == up;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (vec) dtype == DNNS_F32 ? launch_gate_backward<DNNS_F32, false, false>(a, n_sm, st) : launch_gate_backward<DNNS_BF16, false, false>(a, n_sm, st);
-    else if (alias) dtype == DNNS_F32 ? launch_gate_backward<DNNS_F32, true, true>(a, n_sm, st) : launch_gate_backward<DNNS_BF16, true, true>(a, n_sm, st);
-    else dtype == DNNS_F32 ? launch_gate_backward<DNNS_F32, true, false>(a, n_sm, st) : launch_gate_backward<DNNS_BF16, true, false>(a, n_sm, st);
+    if (dtype == DNNS_F32) vec ? launch_gate_backward<DNNS_F32, true>(a, st) : launch_gate_backward<DNNS_F32, false>(a, st);
+    else vec ? launch_gate_backward<DNNS_BF16, true>(a, st) : launch_gate_backward<DNNS_BF16, false>(a, st);
     return cudaGetLastError() == cudaSuccess ? DNNS_OK : DNNS_ERR_CUDA;
 }
 
