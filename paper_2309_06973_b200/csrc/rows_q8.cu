@@ -28,7 +28,7 @@ constexpr uint32_t kNanBits = 0x7FC00000u;
 constexpr int kBlockWarps = 8;  // warps of a block whose teams are single warps
 // Warps of a team at most, by pieces a lane: what keeps a row in registers without spilling.
 constexpr int quantize_warps(int nv) { return nv == 4 ? 16 : 32; }
-constexpr int backward_warps(int nv) { return nv == 1 ? kBlockWarps : nv == 2 ? 9 : 16; }
+constexpr int backward_warps(int nv) { return nv == 4 ? 16 : 8; }
 
 template <int DT>
 struct Store;
@@ -774,7 +774,7 @@ dnns_status run_quantize(const QuantArgs& a, int32_t dtype, void* stream) {
 // columns a lane in registers); 16 warps where 8 do not hold a row.
 Shape norm_backward_shape(int64_t cols) {
     if (cols <= 256) return row_shape(cols, 1, 1);
-    Shape s = row_shape(cols, cols <= 512 * backward_warps(2) ? 2 : 4, 16);
+    Shape s = row_shape(cols, cols <= 512 * backward_warps(2) ? 2 : cols <= 768 * backward_warps(3) ? 3 : 4, 16);
     s.teams = 1;
     return s;
 }
@@ -788,7 +788,7 @@ int64_t norm_backward_slices(int64_t rows, int64_t cols) {
 // Launches the gradient; how many slices of partial sums it writes, or -1.
 template <int DT, bool VEC>
 int64_t launch_norm_backward(const NormBackArgs& a, cudaStream_t st) {
-    static std::atomic<uint64_t> done[3];
+    static std::atomic<uint64_t> done[4];
     constexpr size_t kRoom = 200 * 1024;  // shared memory of an SM that the stages may take
     const Shape s = norm_backward_shape(a.cols);
     const size_t row_bytes = ((size_t)a.cols * (DT == DNNS_F32 ? 4 : 2) + 15) / 16 * 16 + (VEC ? 0 : 16), stage = 3 * row_bytes * s.teams;
@@ -802,9 +802,9 @@ int64_t launch_norm_backward(const NormBackArgs& a, cudaStream_t st) {
     }
     const int64_t grid = std::min<int64_t>((a.rows + s.teams - 1) / s.teams, 148 * blocks);
     const dim3 block(32 * s.warps, s.teams);
-    const auto kernel = s.nv == 1 ? k_norm_backward<DT, VEC, 1> : s.nv == 2 ? k_norm_backward<DT, VEC, 2> : k_norm_backward<DT, VEC, 4>;
+    const auto kernel = s.nv == 1 ? k_norm_backward<DT, VEC, 1> : s.nv == 2 ? k_norm_backward<DT, VEC, 2> : s.nv == 3 ? k_norm_backward<DT, VEC, 3> : k_norm_backward<DT, VEC, 4>;
     int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || !allow_shared(kernel, kRoom, done[s.nv / 2], dev)) return -1;
+    if (cudaGetDevice(&dev) != cudaSuccess || !allow_shared(kernel, kRoom, done[s.nv - 1], dev)) return -1;
     const size_t shared = std::max(stages * stage, s.nv == 1 ? (size_t)kBlockWarps * 256 * sizeof(float) : 0);
     kernel<<<(unsigned)grid, block, shared, st>>>(a, stages, (uint32_t)row_bytes);
     return grid;
