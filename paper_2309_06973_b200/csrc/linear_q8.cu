@@ -47,44 +47,175 @@ __device__ __forceinline__ void store_out(void* y, int64_t at, float v) {
 __device__ __forceinline__ float scaled(int32_t acc, float xs, float ws, float bias) { return fmaf((float)acc * ws, xs, bias); }
 
 // ================= few tokens =================
-// Bytes k0 .. k0 + 15 of a row of k bytes, those past the end as 0 (never read).
-__device__ __forceinline__ int4 row16(const int8_t* row, int32_t k0, int32_t k) {
-    if (k0 + 16 <= k) return *reinterpret_cast<const int4*>(row + k0);
+// Bound by reading the weights once, so what counts is that enough of them are on their way: a warp has R channels, its lanes
+// 16 bytes of each at a time, several loads deep; `parts` warps share a channel's columns where there are few channels.
+// The tokens are read beside them, from the L1 cache but for a block's first warp (the weights pass it by).
+constexpr int kRowsWarps = 8;
+
+__device__ __forceinline__ int4 stream16(const int8_t* p) {
+    int4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ int32_t dot16(const int4& a, const int4& b, int32_t c) { return __dp4a(a.x, b.x, __dp4a(a.y, b.y, __dp4a(a.z, b.z, __dp4a(a.w, b.w, c)))); }
+
+// M tokens at most (a.rows of them), blockIdx.y the token group.
+template <int M, int R, int DT>
+__global__ void __launch_bounds__(32 * kRowsWarps) k_linear_rows(const LinearArgs a, int32_t parts) {
+    constexpr int U = M <= 4 ? 4 : 2;  // loads deep
+    __shared__ int32_t s_part[kRowsWarps][R * M];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int group = warp / parts, part = warp - group * parts;
+    const int32_t n0 = (int32_t)(((int64_t)blockIdx.x * (kRowsWarps / parts) + group) * R);
+    const int32_t t0 = blockIdx.y * M, vecs = a.k >> 4, step = 32 * parts;
+    int32_t acc[R][M];
+    const int8_t *w[R], *x[M];
+#pragma unroll
+    for (int i = 0; i < R; ++i) w[i] = a.wq + (int64_t)min(n0 + i, a.n - 1) * a.ldw;  // (rows past the end repeat the last)
+#pragma unroll
+    for (int t = 0; t < M; ++t) x[t] = a.xq + (int64_t)min(t0 + t, a.rows - 1) * a.ldx;
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int t = 0; t < M; ++t) acc[i][t] = 0;
+    int32_t v = part * 32 + lane;
+    for (; v + (U - 1) * step < vecs; v += U * step) {
+        int4 wv[U][R];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < R; ++i) wv[u][i] = stream16(w[i] + 16 * (v + u * step));
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int t = 0; t < M; ++t) {
+                const int4 xv = __ldg(reinterpret_cast<const int4*>(x[t] + 16 * (v + u * step)));
+#pragma unroll
+                for (int i = 0; i < R; ++i) acc[i][t] = dot16(wv[u][i], xv, acc[i][t]);
+            }
+    }
+    for (; v < vecs; v += step) {
+        int4 wv[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) wv[i] = stream16(w[i] + 16 * v);
+#pragma unroll
+        for (int t = 0; t < M; ++t) {
+            const int4 xv = __ldg(reinterpret_cast<const int4*>(x[t] + 16 * v));
+#pragma unroll
+            for (int i = 0; i < R; ++i) acc[i][t] = dot16(wv[i], xv, acc[i][t]);
+        }
+    }
+    // the last columns, fewer than 16: a lane each
+    if (const int32_t c = (vecs << 4) + lane; part == 0 && c < a.k) {
+#pragma unroll
+        for (int t = 0; t < M; ++t)
+#pragma unroll
+            for (int i = 0; i < R; ++i) acc[i][t] += (int32_t)w[i][c] * (int32_t)x[t][c];
+    }
+    // lane l ends up with the l-th of the R * M sums (32 at a time)
+    constexpr int kSums = R * M;
+    int32_t mine[(kSums + 31) / 32];
+#pragma unroll
+    for (int q = 0; q < kSums; ++q) {
+        const int32_t sum = __reduce_add_sync(kFullMask, acc[q / M][q % M]);
+        if (lane == (q & 31)) mine[q >> 5] = sum;
+    }
+    if (parts > 1) {
+#pragma unroll
+        for (int b = 0; b < (kSums + 31) / 32; ++b)
+            if (b * 32 + lane < kSums) s_part[warp][b * 32 + lane] = mine[b];
+        __syncthreads();
+        if (part) return;
+#pragma unroll
+        for (int b = 0; b < (kSums + 31) / 32; ++b)
+            if (b * 32 + lane < kSums)
+                for (int i = 1; i < parts; ++i) mine[b] += s_part[warp + i][b * 32 + lane];
+    }
+#pragma unroll
+    for (int b = 0; b < (kSums + 31) / 32; ++b) {
+        const int q = b * 32 + lane, n = n0 + q / M, t = t0 + q % M;
+        if (q < kSums && n < a.n && t < a.rows)
+            store_out<DT>(a.y, (int64_t)t * a.ldy + n, scaled(mine[b], a.xscale[t], a.wscale[n], a.bias ? a.bias[n] : 0.0f));
+    }
+}
+
+// ================= a few more tokens: warp-wide products =================
+// Still bound by reading the weights once, but with dot products lane by lane the tokens, read once a channel, become the larger
+// traffic (L1).  A warp-wide product of 16 channels x 32 columns by 8 tokens reads them once for 16 channels.  The sum over the
+// columns may go in any order, so a lane feeds the product with 16 neighbouring bytes of a row at a time: lane (g, q) has
+// bytes 16 q .. of 64 of channels g and g + 8 and of token g, words 0, 1 for one product and 2, 3 for the next.  `parts` warps
+// share the columns of a group of 16 channels and meet in shared memory.
+__device__ __forceinline__ void warp_product(int32_t (&d)[4], int32_t a0, int32_t a1, int32_t a2, int32_t a3, int32_t b0, int32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void lane_product(int32_t (&d)[4], const int4& lo, const int4& hi, const int4& x) {
+    warp_product(d, lo.x, hi.x, lo.y, hi.y, x.x, x.y);
+    warp_product(d, lo.z, hi.z, lo.w, hi.w, x.z, x.w);
+}
+// Bytes c .. c + 15 of a row of k bytes, those past the end as 0 (never read).
+__device__ __forceinline__ int4 row16(const int8_t* row, int32_t c, int32_t k) {
+    if (c + 16 <= k) return *reinterpret_cast<const int4*>(row + c);
     uint32_t w[4] = {0, 0, 0, 0};
-    for (int i = 0; k0 + i < k; ++i) w[i >> 2] |= (uint32_t)(uint8_t)row[k0 + i] << (8 * (i & 3));
+    for (int i = 0; c + i < k; ++i) w[i >> 2] |= (uint32_t)(uint8_t)row[c + i] << (8 * (i & 3));
     return make_int4((int)w[0], (int)w[1], (int)w[2], (int)w[3]);
 }
 
-constexpr int kTokens = 8;    // tokens of a block
-constexpr int kRowsWarp = 4;  // output channels of a warp
-
-template <int DT>
-__global__ void __launch_bounds__(256) k_linear_rows(const LinearArgs a) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t n0 = ((int64_t)blockIdx.x * 8 + warp) * kRowsWarp;
-    const int32_t t0 = blockIdx.y * kTokens;
-    int32_t acc[kRowsWarp][kTokens] = {};
-    for (int32_t k0 = lane * 16; k0 < a.k; k0 += 512) {
-        int4 x[kTokens];
+// 8 * TB tokens at most (a.rows of them)
+template <int TB, int DT>
+__global__ void __launch_bounds__(32 * kRowsWarps, 2) k_linear_few(const LinearArgs a, int32_t parts) {
+    constexpr int U = 4, kSums = 16 * 8 * TB;  // loads deep; results of a group
+    __shared__ int32_t s_part[kRowsWarps][kSums];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
+    const int groups = kRowsWarps / parts, group = warp / parts, part = warp - group * parts;
+    const int32_t n0 = (int32_t)(((int64_t)blockIdx.x * groups + group) * 16);
+    const int8_t* lo = a.wq + (int64_t)min(n0 + g, a.n - 1) * a.ldw;  // (rows and tokens past the end repeat the last)
+    const int8_t* hi = a.wq + (int64_t)min(n0 + g + 8, a.n - 1) * a.ldw;
+    const int8_t* x[TB];
 #pragma unroll
-        for (int t = 0; t < kTokens; ++t) x[t] = t0 + t < a.rows ? row16(a.xq + (int64_t)(t0 + t) * a.ldx, k0, a.k) : make_int4(0, 0, 0, 0);
+    for (int t = 0; t < TB; ++t) x[t] = a.xq + (int64_t)min(8 * t + g, a.rows - 1) * a.ldx;
+    int32_t acc[TB][4];
 #pragma unroll
-        for (int i = 0; i < kRowsWarp; ++i) {
-            if (n0 + i >= a.n) break;
-            const int4 w = row16(a.wq + (n0 + i) * a.ldw, k0, a.k);
+    for (int t = 0; t < TB; ++t)
 #pragma unroll
-            for (int t = 0; t < kTokens; ++t)
-                acc[i][t] = __dp4a(w.x, x[t].x, __dp4a(w.y, x[t].y, __dp4a(w.z, x[t].z, __dp4a(w.w, x[t].w, acc[i][t]))));
-        }
+        for (int i = 0; i < 4; ++i) acc[t][i] = 0;
+    const int32_t whole = a.k >> 6, step = parts;  // pieces of 64 columns
+    int32_t b = part;
+    for (; b + (U - 1) * step < whole; b += U * step) {
+        int4 wl[U], wh[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) wl[u] = stream16(lo + 64 * (b + u * step) + 16 * q), wh[u] = stream16(hi + 64 * (b + u * step) + 16 * q);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int t = 0; t < TB; ++t) lane_product(acc[t], wl[u], wh[u], __ldg(reinterpret_cast<const int4*>(x[t] + 64 * (b + u * step) + 16 * q)));
     }
+    for (; b < whole; b += step) {
+        const int4 wl = stream16(lo + 64 * b + 16 * q), wh = stream16(hi + 64 * b + 16 * q);
 #pragma unroll
-    for (int i = 0; i < kRowsWarp; ++i)
+        for (int t = 0; t < TB; ++t) lane_product(acc[t], wl, wh, __ldg(reinterpret_cast<const int4*>(x[t] + 64 * b + 16 * q)));
+    }
+    if (part == parts - 1 && (a.k & 63)) {
+        const int32_t c = 64 * whole + 16 * q;
+        const int4 wl = row16(lo, c, a.k), wh = row16(hi, c, a.k);
 #pragma unroll
-        for (int t = 0; t < kTokens; ++t) {
-            const int32_t s = __reduce_add_sync(kFullMask, acc[i][t]);
-            if (lane == 0 && n0 + i < a.n && t0 + t < a.rows)
-                store_out<DT>(a.y, (int64_t)(t0 + t) * a.ldy + n0 + i, scaled(s, a.xscale[t0 + t], a.wscale[n0 + i], a.bias ? a.bias[n0 + i] : 0.0f));
-        }
+        for (int t = 0; t < TB; ++t) lane_product(acc[t], wl, wh, row16(x[t], c, a.k));
+    }
+    // sum [token][channel] of the group
+#pragma unroll
+    for (int t = 0; t < TB; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s_part[warp][(8 * t + 2 * q + (i & 1)) * 16 + g + 8 * (i >> 1)] = acc[t][i];
+    __syncthreads();
+    for (int i = threadIdx.x; i < groups * kSums; i += 32 * kRowsWarps) {
+        const int grp = i / kSums, at = i - grp * kSums, t = at >> 4;
+        const int32_t n = (int32_t)(((int64_t)blockIdx.x * groups + grp) * 16) + (at & 15);
+        if (t >= a.rows || n >= a.n) continue;
+        int32_t sum = 0;
+        for (int p = 0; p < parts; ++p) sum += s_part[grp * parts + p][at];
+        store_out<DT>(a.y, (int64_t)t * a.ldy + n, scaled(sum, a.xscale[t], a.wscale[n], a.bias ? a.bias[n] : 0.0f));
+    }
 }
 
 // ================= tensor cores: the pieces both tile kernels are made of =================
@@ -603,16 +734,44 @@ bool launch_pair(const LinearArgs& a, int n_sm, int dev, cudaStream_t st) {
     return true;
 }
 
-template <int DT>
-bool launch_rows(const LinearArgs& a, cudaStream_t st) {
-    const int64_t step = 8 * kRowsWarp, most = 65535 * (int64_t)kTokens;  // (the grid's second extent)
+template <int M, int DT>
+void launch_rows_of(const LinearArgs& a, int n_sm, cudaStream_t st) {
+    // two channels a warp where that still leaves a dozen warps an SM (each then has more loads on their way), and warps that
+    // share a channel where there are too few channels, down to four loads a lane
+    const bool two = a.n >= 24 * n_sm;
+    int parts = 1;
+    while (parts < kRowsWarps && (int64_t)a.n * parts < 12 * (int64_t)n_sm && a.k >= 4 * 512 * 2 * parts) parts *= 2;
+    const int64_t step = kRowsWarps / parts * (two ? 2 : 1), most = 65535 * (int64_t)M;  // (the grid's second extent)
     for (int64_t t0 = 0; t0 < a.rows; t0 += most) {
         LinearArgs part = a;
         part.rows = (int32_t)std::min<int64_t>(a.rows - t0, most);
         part.xq += t0 * a.ldx, part.xscale += t0;
         part.y = static_cast<char*>(a.y) + t0 * a.ldy * (DT == DNNS_F32 ? 4 : 2);
-        const dim3 grid((unsigned)((a.n + step - 1) / step), (unsigned)((part.rows + kTokens - 1) / kTokens));
-        k_linear_rows<DT><<<grid, 256, 0, st>>>(part);
+        const dim3 grid((unsigned)((a.n + step - 1) / step), (unsigned)((part.rows + M - 1) / M));
+        if (two) k_linear_rows<M, 2, DT><<<grid, 32 * kRowsWarps, 0, st>>>(part, parts);
+        else k_linear_rows<M, 1, DT><<<grid, 32 * kRowsWarps, 0, st>>>(part, parts);
+    }
+}
+
+template <int DT>
+bool launch_rows(const LinearArgs& a, int n_sm, cudaStream_t st) {
+    if (a.rows <= 1) launch_rows_of<1, DT>(a, n_sm, st);
+    else if (a.rows <= 2) launch_rows_of<2, DT>(a, n_sm, st);
+    else launch_rows_of<4, DT>(a, n_sm, st);
+    return true;
+}
+
+template <int DT>
+bool launch_few(const LinearArgs& a, int n_sm, cudaStream_t st) {
+    const int64_t groups = ((int64_t)a.n + 15) / 16;
+    int parts = 1;
+    while (parts < kRowsWarps && groups * parts < 16 * (int64_t)n_sm && a.k >= 4 * 64 * 2 * parts) parts *= 2;
+    const unsigned grid = (unsigned)((groups * parts + kRowsWarps - 1) / kRowsWarps);
+    switch ((a.rows + 7) / 8) {
+        case 1: k_linear_few<1, DT><<<grid, 32 * kRowsWarps, 0, st>>>(a, parts); break;
+        case 2: k_linear_few<2, DT><<<grid, 32 * kRowsWarps, 0, st>>>(a, parts); break;
+        case 3: k_linear_few<3, DT><<<grid, 32 * kRowsWarps, 0, st>>>(a, parts); break;
+        default: k_linear_few<4, DT><<<grid, 32 * kRowsWarps, 0, st>>>(a, parts); break;
     }
     return true;
 }
@@ -623,7 +782,8 @@ struct Choice {
 };
 
 Choice choose(const LinearArgs& a, int n_sm) {
-    if (a.k == 0 || a.rows <= 8) return {0, 0, 1};
+    if (a.k == 0 || a.rows <= 1) return {0, 0, 1};
+    if (a.rows <= 32) return {8, 0, 1};
     const int64_t channels = (a.n + kTileRows - 1) / kTileRows, blocks = (a.k + kBlockK - 1) / kBlockK;
     auto tiles = [&](int bt) { return channels * ((a.rows + bt - 1) / bt); };
     if (a.rows > 128 && tiles(256) >= n_sm) return {256, 1, 1};
@@ -635,7 +795,8 @@ Choice choose(const LinearArgs& a, int n_sm) {
 
 template <int DT>
 bool launch_linear(const LinearArgs& a, const Choice& c, int n_sm, int dev, cudaStream_t st) {
-    if (c.tokens == 0) return launch_rows<DT>(a, st);
+    if (c.tokens == 0) return launch_rows<DT>(a, n_sm, st);
+    if (c.tokens == 8) return launch_few<DT>(a, n_sm, st);
     if (c.pair) return c.tokens == 256 ? launch_pair<256, DT>(a, n_sm, dev, st) : launch_pair<128, DT>(a, n_sm, dev, st);
     switch (c.tokens) {
         case 32: return launch_tile<32, DT>(a, c.split, dev, st);
