@@ -320,6 +320,25 @@ struct FoldJob {
 int launch_fold(const Tables& tb, void* arena, const uint64_t* offsets, const int32_t* shapes, uint32_t* job_count,
                 FoldJob* jobs, int n_sm, cudaStream_t st);
 cudaError_t init_kernel_attributes();
+// Launch of a kernel that may begin before the kernel in front of it in the stream has ended: it has chain_wait() before its first
+// access to global memory, so only its set-up (and the launch itself) overlaps, and chain_go() to let the next one do the same.
+// Small kernels in a row cost 1 to 2 us less each.  Every thread of such a kernel waits, so that its end means the end of all before it.
+template <typename... P, typename... A>
+inline bool launch_chained(void (*kernel)(P...), dim3 grid, dim3 block, size_t shared, cudaStream_t st, unsigned cluster, A&&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid, cfg.blockDim = block, cfg.dynamicSmemBytes = shared, cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = cluster, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
+    cfg.attrs = at, cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, P(args)...) == cudaSuccess;
+}
+#ifdef __CUDACC__
+__device__ __forceinline__ void chain_go() { asm volatile("griddepcontrol.launch_dependents;"); }
+__device__ __forceinline__ void chain_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+#endif
 // Lets a kernel use `bytes` of dynamic shared memory, once per device (`done`: a static word of the caller, a bit per device).
 template <typename F>
 inline bool allow_shared(F* kernel, size_t bytes, std::atomic<uint64_t>& done, int dev) {

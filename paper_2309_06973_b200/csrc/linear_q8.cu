@@ -62,6 +62,8 @@ __device__ __forceinline__ int32_t dot16(const int4& a, const int4& b, int32_t c
 // M tokens at most (a.rows of them), blockIdx.y the token group.
 template <int M, int R, int DT>
 __global__ void __launch_bounds__(32 * kRowsWarps) k_linear_rows(const LinearArgs a, int32_t parts) {
+    chain_go();
+    chain_wait();
     constexpr int U = M <= 4 ? 4 : 2;  // loads deep
     __shared__ int32_t s_part[kRowsWarps][R * M];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -165,6 +167,8 @@ __device__ __forceinline__ int4 row16(const int8_t* row, int32_t c, int32_t k) {
 // 8 * TB tokens at most (a.rows of them)
 template <int TB, int DT>
 __global__ void __launch_bounds__(32 * kRowsWarps, 2) k_linear_few(const LinearArgs a, int32_t parts) {
+    chain_go();
+    chain_wait();
     constexpr int U = 4, kSums = 16 * 8 * TB;  // loads deep; results of a group
     __shared__ int32_t s_part[kRowsWarps][kSums];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
@@ -414,6 +418,8 @@ __global__ void __launch_bounds__(kTileThreads2) k_linear_tile(const LinearArgs 
     }
     __syncthreads();
     mma_fence_after();
+    chain_go();  // (not before this CTA has its tensor memory: the next kernel's CTAs would take it and wait for this one's end)
+    chain_wait();
     const uint32_t tmem = s.tmem;
     volatile uint32_t* gave_up = &s.gave_up;
 
@@ -534,7 +540,7 @@ struct PairCfg {
 };
 
 template <int BT, int DT>
-__global__ void __launch_bounds__(kPairThreads) __cluster_dims__(2, 1, 1)
+__global__ void __launch_bounds__(kPairThreads)
     k_linear_pair(const LinearArgs a, const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap) {
     typedef PairCfg<BT> Cfg;
     unsigned char* base = shared_base();
@@ -572,6 +578,8 @@ __global__ void __launch_bounds__(kPairThreads) __cluster_dims__(2, 1, 1)
     __syncthreads();
     cluster_sync();  // the other CTA's barriers are ready
     mma_fence_after();
+    chain_go();  // (not before this CTA has its tensor memory: the next kernel's CTAs would take it and wait for this one's end)
+    chain_wait();
     const uint32_t tmem = s.tmem;
     volatile uint32_t* gave_up = &s.gave_up;
     bool lost = false;
@@ -709,16 +717,8 @@ bool launch_tile(const LinearArgs& a, int split, int dev, cudaStream_t st) {
     CUtensorMap wmap, xmap;
     if (!make_map(&wmap, a.wq, a.n, a.k, a.ldw, kTileRows) || !make_map(&xmap, a.xq, a.rows, a.k, a.ldx, BT)) return false;
     const int32_t t_tiles = (a.rows + BT - 1) / BT, n_tiles = (a.n + kTileRows - 1) / kTileRows;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((int64_t)t_tiles * n_tiles * split));
-    cfg.blockDim = dim3(kTileThreads2);
-    cfg.dynamicSmemBytes = Cfg::kShared;
-    cfg.stream = st;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = (unsigned)split, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
-    cfg.attrs = at, cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, k_linear_tile<BT, DT>, a, wmap, xmap, t_tiles, (int32_t)split) == cudaSuccess;
+    return launch_chained(k_linear_tile<BT, DT>, (unsigned)((int64_t)t_tiles * n_tiles * split), kTileThreads2, Cfg::kShared, st, (unsigned)split, a, wmap, xmap, t_tiles,
+                          (int32_t)split);
 }
 
 template <int BT, int DT>
@@ -730,12 +730,11 @@ bool launch_pair(const LinearArgs& a, int n_sm, int dev, cudaStream_t st) {
     if (!make_map(&wmap, a.wq, a.n, a.k, a.ldw, kTileRows) || !make_map(&xmap, a.xq, a.rows, a.k, a.ldx, BT / 2)) return false;
     const int64_t tiles = (int64_t)((a.rows + BT - 1) / BT) * ((a.n + 2 * kTileRows - 1) / (2 * kTileRows));
     const unsigned grid = 2 * (unsigned)std::min<int64_t>(tiles, n_sm / 2);
-    k_linear_pair<BT, DT><<<grid, kPairThreads, Cfg::kShared, st>>>(a, wmap, xmap);
-    return true;
+    return launch_chained(k_linear_pair<BT, DT>, grid, kPairThreads, Cfg::kShared, st, 2, a, wmap, xmap);
 }
 
 template <int M, int DT>
-void launch_rows_of(const LinearArgs& a, int n_sm, cudaStream_t st) {
+bool launch_rows_of(const LinearArgs& a, int n_sm, cudaStream_t st) {
     // two channels a warp where that still leaves a dozen warps an SM (each then has more loads on their way), and warps that
     // share a channel where there are too few channels, down to four loads a lane
     const bool two = a.n >= 24 * n_sm;
@@ -748,17 +747,15 @@ void launch_rows_of(const LinearArgs& a, int n_sm, cudaStream_t st) {
         part.xq += t0 * a.ldx, part.xscale += t0;
         part.y = static_cast<char*>(a.y) + t0 * a.ldy * (DT == DNNS_F32 ? 4 : 2);
         const dim3 grid((unsigned)((a.n + step - 1) / step), (unsigned)((part.rows + M - 1) / M));
-        if (two) k_linear_rows<M, 2, DT><<<grid, 32 * kRowsWarps, 0, st>>>(part, parts);
-        else k_linear_rows<M, 1, DT><<<grid, 32 * kRowsWarps, 0, st>>>(part, parts);
+        if (!launch_chained(two ? k_linear_rows<M, 2, DT> : k_linear_rows<M, 1, DT>, grid, 32 * kRowsWarps, 0, st, 1, part, parts)) return false;
     }
+    return true;
 }
 
 template <int DT>
 bool launch_rows(const LinearArgs& a, int n_sm, cudaStream_t st) {
-    if (a.rows <= 1) launch_rows_of<1, DT>(a, n_sm, st);
-    else if (a.rows <= 2) launch_rows_of<2, DT>(a, n_sm, st);
-    else launch_rows_of<4, DT>(a, n_sm, st);
-    return true;
+    if (a.rows <= 1) return launch_rows_of<1, DT>(a, n_sm, st);
+    return a.rows <= 2 ? launch_rows_of<2, DT>(a, n_sm, st) : launch_rows_of<4, DT>(a, n_sm, st);
 }
 
 template <int DT>
@@ -767,13 +764,9 @@ bool launch_few(const LinearArgs& a, int n_sm, cudaStream_t st) {
     int parts = 1;
     while (parts < kRowsWarps && groups * parts < 16 * (int64_t)n_sm && a.k >= 4 * 64 * 2 * parts) parts *= 2;
     const unsigned grid = (unsigned)((groups * parts + kRowsWarps - 1) / kRowsWarps);
-    switch ((a.rows + 7) / 8) {
-        case 1: k_linear_few<1, DT><<<grid, 32 * kRowsWarps, 0, st>>>(a, parts); break;
-        case 2: k_linear_few<2, DT><<<grid, 32 * kRowsWarps, 0, st>>>(a, parts); break;
-        case 3: k_linear_few<3, DT><<<grid, 32 * kRowsWarps, 0, st>>>(a, parts); break;
-        default: k_linear_few<4, DT><<<grid, 32 * kRowsWarps, 0, st>>>(a, parts); break;
-    }
-    return true;
+    const int blocks = (a.rows + 7) / 8;
+    const auto kernel = blocks == 1 ? k_linear_few<1, DT> : blocks == 2 ? k_linear_few<2, DT> : blocks == 3 ? k_linear_few<3, DT> : k_linear_few<4, DT>;
+    return launch_chained(kernel, grid, 32 * kRowsWarps, 0, st, 1, a, parts);
 }
 
 // Which kernel: `tokens` of a tile (0: k_linear_rows), over one CTA or a pair, columns split so many ways.

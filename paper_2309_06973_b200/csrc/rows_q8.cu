@@ -290,6 +290,8 @@ __device__ __forceinline__ void store_quantized(const QuantArgs& a, int64_t r, i
 // blockDim: (32 * warps of a team, teams); more than one team only of one warp
 template <int OP, int DT, bool VEC, int NV>
 __global__ void __launch_bounds__(32 * quantize_warps(NV)) k_rows_quantize(const QuantArgs a) {
+    chain_go();
+    chain_wait();
     typedef typename Store<DT>::type T;
     __shared__ uint32_t s_scratch[64];
     const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5;
@@ -388,17 +390,18 @@ Shape row_shape(int64_t cols, int nv, int max_warps) {
 }
 
 template <int OP, int DT, bool VEC>
-void launch_quantize(const QuantArgs& a, int n_sm, cudaStream_t st) {
+bool launch_quantize(const QuantArgs& a, int n_sm, cudaStream_t st) {
     // few rows, or short ones: as many warps as a row feeds; else more bytes in flight a lane
     Shape s{0, 0, 0};
     for (int nv = a.rows <= n_sm || a.cols <= 256 ? 1 : a.cols <= 512 ? 2 : 4; nv <= 4 && s.nv == 0; nv *= 2) s = row_shape(a.cols, nv, quantize_warps(nv));
     if (s.nv == 0) s.warps = quantize_warps(0);
     const dim3 block(32 * s.warps, s.teams);
     const unsigned grid = (unsigned)((a.rows + s.teams - 1) / s.teams);
-    if (s.nv == 0) k_rows_quantize<OP, DT, VEC, 0><<<grid, block, 0, st>>>(a);
-    else if (s.nv == 1) k_rows_quantize<OP, DT, VEC, 1><<<grid, block, 0, st>>>(a);
-    else if (s.nv == 2) k_rows_quantize<OP, DT, VEC, 2><<<grid, block, 0, st>>>(a);
-    else k_rows_quantize<OP, DT, VEC, 4><<<grid, block, 0, st>>>(a);
+    const auto kernel = s.nv == 0   ? k_rows_quantize<OP, DT, VEC, 0>
+                        : s.nv == 1 ? k_rows_quantize<OP, DT, VEC, 1>
+                        : s.nv == 2 ? k_rows_quantize<OP, DT, VEC, 2>
+                                    : k_rows_quantize<OP, DT, VEC, 4>;
+    return launch_chained(kernel, grid, block, 0, st, 1, a);
 }
 
 // ---- gradients -------------------------------------------------------------------------------------------------
@@ -499,6 +502,8 @@ __device__ __forceinline__ void staged8(const T* row, const unsigned char* stage
 // than one team only of one warp.
 template <int DT, bool VEC, int NV>
 __global__ void __launch_bounds__(32 * backward_warps(NV), NV == 4 ? 1 : 2) k_norm_backward(const NormBackArgs a, int stages, uint32_t row_bytes) {
+    chain_go();
+    chain_wait();
     typedef typename Store<DT>::type T;
     extern __shared__ __align__(16) unsigned char s_rows[];  // [teams of the block][stages][3][row_bytes]
     __shared__ __align__(16) float2 s_scratch[2][16];
@@ -610,6 +615,8 @@ __global__ void __launch_bounds__(32 * backward_warps(NV), NV == 4 ? 1 : 2) k_no
 // The same for rows that do not fit in shared memory: walked twice, the partial sums in the team's slice of the workspace.
 template <int DT, bool VEC>
 __global__ void __launch_bounds__(512) k_norm_backward_long(const NormBackArgs a) {
+    chain_go();
+    chain_wait();
     typedef typename Store<DT>::type T;
     __shared__ __align__(16) float2 s_scratch[2][16];
     const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5;
@@ -663,6 +670,8 @@ __global__ void __launch_bounds__(512) k_norm_backward_long(const NormBackArgs a
 
 // dweight[c] = sum of the teams' partial sums in a fixed order: 8 columns (a sector) by 32 runs of teams a block.
 __global__ void __launch_bounds__(256) k_norm_weight_sum(const float* __restrict__ part, int64_t teams, int64_t cols, float* __restrict__ dweight) {
+    chain_go();
+    chain_wait();
     __shared__ float s[32][9];
     const int64_t c0 = (int64_t)blockIdx.x * 8;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = threadIdx.x & 7, run = threadIdx.x >> 3;
@@ -690,6 +699,8 @@ struct GateBackArgs {
 // blockIdx.x: rows, by teams of a block; blockIdx.y: pieces of a row, by warps of a team.
 template <int DT, bool VEC>
 __global__ void __launch_bounds__(32 * kBlockWarps) k_gate_backward(const GateBackArgs a) {
+    chain_go();
+    chain_wait();
     typedef typename Store<DT>::type T;
     const int cols = (int)a.cols, warps = blockDim.x >> 5, warp = threadIdx.x >> 5;
     for (int64_t r = (int64_t)blockIdx.x * blockDim.y + threadIdx.y; r < a.rows; r += (int64_t)gridDim.x * blockDim.y) {
@@ -765,9 +776,9 @@ dnns_status run_quantize(const QuantArgs& a, int32_t dtype, void* stream) {
     const size_t e = elem_bytes(dtype);
     const bool vec = on_16(a.x, a.ldx, a.rows, e) && (!a.x2 || on_16(a.x2, a.ldx2, a.rows, e)) && (!a.h || on_16(a.h, a.ldh, a.rows, e)) &&
                      (!a.values || on_16(a.values, a.ldv, a.rows, 2)) && (!a.weight || on_16(a.weight, 0, 1, 4));
-    if (dtype == DNNS_F32) vec ? launch_quantize<OP, DNNS_F32, true>(a, n_sm, st) : launch_quantize<OP, DNNS_F32, false>(a, n_sm, st);
-    else vec ? launch_quantize<OP, DNNS_BF16, true>(a, n_sm, st) : launch_quantize<OP, DNNS_BF16, false>(a, n_sm, st);
-    return cudaGetLastError() == cudaSuccess ? DNNS_OK : DNNS_ERR_CUDA;
+    const bool launched = dtype == DNNS_F32 ? (vec ? launch_quantize<OP, DNNS_F32, true>(a, n_sm, st) : launch_quantize<OP, DNNS_F32, false>(a, n_sm, st))
+                                            : (vec ? launch_quantize<OP, DNNS_BF16, true>(a, n_sm, st) : launch_quantize<OP, DNNS_BF16, false>(a, n_sm, st));
+    return launched && cudaGetLastError() == cudaSuccess ? DNNS_OK : DNNS_ERR_CUDA;
 }
 
 // Warps of a team of the norm's gradient: NV = 2 up to 4096 columns, 4 above (fewer warps, but the weights and sums of 8 more
@@ -797,8 +808,7 @@ int64_t launch_norm_backward(const NormBackArgs& a, cudaStream_t st) {
     const int stages = (int)std::min<size_t>(4, kRoom / blocks / stage);
     if (s.nv == 0 || stages < 2) {
         const int64_t grid = std::min<int64_t>(a.rows, 148);
-        k_norm_backward_long<DT, VEC><<<(unsigned)grid, 512, 0, st>>>(a);
-        return grid;
+        return launch_chained(k_norm_backward_long<DT, VEC>, (unsigned)grid, 512, 0, st, 1, a) ? grid : -1;
     }
     const int64_t grid = std::min<int64_t>((a.rows + s.teams - 1) / s.teams, 148 * blocks);
     const dim3 block(32 * s.warps, s.teams);
@@ -806,16 +816,15 @@ int64_t launch_norm_backward(const NormBackArgs& a, cudaStream_t st) {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || !allow_shared(kernel, kRoom, done[s.nv - 1], dev)) return -1;
     const size_t shared = std::max(stages * stage, s.nv == 1 ? (size_t)kBlockWarps * 256 * sizeof(float) : 0);
-    kernel<<<(unsigned)grid, block, shared, st>>>(a, stages, (uint32_t)row_bytes);
-    return grid;
+    return launch_chained(kernel, (unsigned)grid, block, shared, st, 1, a, stages, (uint32_t)row_bytes) ? grid : -1;
 }
 
 template <int DT, bool VEC>
-void launch_gate_backward(const GateBackArgs& a, cudaStream_t st) {
+bool launch_gate_backward(const GateBackArgs& a, cudaStream_t st) {
     Shape s = row_shape(a.cols, 1, kBlockWarps);
     const int rounds = (int)((a.cols + 256 * s.warps - 1) / (256 * s.warps));
     const dim3 grid((unsigned)std::min<int64_t>((a.rows + s.teams - 1) / s.teams, (int64_t)1 << 30), std::min(rounds, 65535));
-    k_gate_backward<DT, VEC><<<grid, dim3(32 * s.warps, s.teams), 0, st>>>(a);
+    return launch_chained(k_gate_backward<DT, VEC>, grid, dim3(32 * s.warps, s.teams), 0, st, 1, a);
 }
 
 bool eps_ok(float eps) { return eps >= 0x1p-126f && eps <= 3.402823466e38f; }
@@ -882,7 +891,7 @@ dnns_status dnns_rmsnorm_backward(const void* dy, int64_t lddy, const void* h, i
     const int64_t slices = dtype == DNNS_F32 ? (vec ? launch_norm_backward<DNNS_F32, true>(a, st) : launch_norm_backward<DNNS_F32, false>(a, st))
                                             : (vec ? launch_norm_backward<DNNS_BF16, true>(a, st) : launch_norm_backward<DNNS_BF16, false>(a, st));
     if (slices < 0) return DNNS_ERR_CUDA;
-    if (dweight) k_norm_weight_sum<<<(unsigned)((cols + 7) / 8), 256, 0, st>>>(a.part, slices, cols, dweight);
+    if (dweight && !launch_chained(k_norm_weight_sum, (unsigned)((cols + 7) / 8), 256, 0, st, 1, a.part, slices, cols, dweight)) return DNNS_ERR_CUDA;
     return cudaGetLastError() == cudaSuccess ? DNNS_OK : DNNS_ERR_CUDA;
 }
 
@@ -903,9 +912,9 @@ dnns_status dnns_silu_gate_backward(const void* dy, int64_t lddy, const void* ga
     const bool vec = on_16(dy, lddy, rows, e) && on_16(gate, ldg, rows, e) && on_16(up, ldu, rows, e) && on_16(dgate, lddg, rows, e) &&
                      on_16(dup, lddu, rows, e);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (dtype == DNNS_F32) vec ? launch_gate_backward<DNNS_F32, true>(a, st) : launch_gate_backward<DNNS_F32, false>(a, st);
-    else vec ? launch_gate_backward<DNNS_BF16, true>(a, st) : launch_gate_backward<DNNS_BF16, false>(a, st);
-    return cudaGetLastError() == cudaSuccess ? DNNS_OK : DNNS_ERR_CUDA;
+    const bool launched = dtype == DNNS_F32 ? (vec ? launch_gate_backward<DNNS_F32, true>(a, st) : launch_gate_backward<DNNS_F32, false>(a, st))
+                                            : (vec ? launch_gate_backward<DNNS_BF16, true>(a, st) : launch_gate_backward<DNNS_BF16, false>(a, st));
+    return launched && cudaGetLastError() == cudaSuccess ? DNNS_OK : DNNS_ERR_CUDA;
 }
 
 }  // extern "C"
