@@ -256,7 +256,7 @@ __device__ __forceinline__ bool mbar_try(uint64_t* bar, uint32_t parity) {
     uint32_t done;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"  // may sleep up to the hint (ns)
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"  // may sleep up to the hint (ns) before it answers
         "selp.u32 %0, 1, 0, p;\n\t}"
         : "=r"(done)
         : "r"(smem_addr(bar)), "r"(parity), "r"(20000u)
@@ -269,15 +269,19 @@ __device__ __forceinline__ uint64_t global_ns() {
     return t;
 }
 // Wait for a phase of an mbarrier, but not for ever: false when the wait was given up, or another thread of the CTA gave
-// up before.
+// up before.  (The timer takes long to read: it is looked at only after many tries.)
 __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volatile uint32_t* gave_up) {
     if (mbar_try(bar, parity)) return true;
-    const uint64_t t0 = global_ns();
+    uint64_t since = 0;
     for (uint32_t spin = 1;; ++spin) {
         if (mbar_try(bar, parity)) return true;
-        if ((spin & 15u) == 0 && (*gave_up || global_ns() - t0 > kWaitLimitNs)) {
-            *gave_up = 1;
-            return false;
+        if ((spin & 15u) == 0) {
+            const uint64_t now = global_ns();
+            if (since == 0) since = now;
+            if (*gave_up || now - since > kWaitLimitNs) {
+                *gave_up = 1;
+                return false;
+            }
         }
     }
 }
@@ -366,7 +370,7 @@ __device__ __forceinline__ void store_columns(const LinearArgs& a, const int32_t
 }
 
 struct TileShared {  // in front of the stages
-    uint64_t full[8], empty[8], done[2], taken[2], drain;
+    uint64_t full[10], empty[10], done[2], taken[2], drain;
     uint32_t tmem, gave_up;
 };
 constexpr uint32_t kSharedHead = 1024;
@@ -383,10 +387,13 @@ constexpr int kTileThreads2 = 192;  // warp 0 loads, warp 1 issues the products,
 template <int BT>
 struct TileCfg {
     static constexpr uint32_t kStage = kWeightBytes + BT * kBlockK;
-    static constexpr int kStages = BT <= 32 ? 5 : BT <= 64 ? 4 : BT <= 128 ? 6 : 4;
+    #ifndef ST32
+#define ST32 5
+#endif
+    static constexpr int kStages = BT <= 32 ? ST32 : BT <= 64 ? 4 : 6;
     static constexpr uint32_t kShared = kSharedHead + kStages * kStage + 1024;
     static constexpr uint32_t kColumns = BT;
-    static_assert(kStages <= 8 && kStages * kStage >= BT * kTileRows * 4, "the partial sums of a cluster reuse the stages");
+    static_assert(kStages <= 10 && kStages * kStage >= BT * kTileRows * 4, "the partial sums of a cluster reuse the stages");
 };
 
 template <int BT, int DT>
@@ -469,7 +476,7 @@ __global__ void __launch_bounds__(kTileThreads2) k_linear_tile(const LinearArgs 
     }
     // everybody waits for the sums: after this no copy and no product of this CTA is in flight
     __syncwarp();
-    const bool ok = mbar_wait(&s.done[0], 0, gave_up);
+    const bool ok = __shfl_sync(kFullMask, (int)(lane == 0 && mbar_wait(&s.done[0], 0, gave_up)), 0);
     mma_fence_after();
     const int quarter = warp & 3;  // tensor memory lanes a warp may read: 32 * (its index mod 4) ..
     const int32_t n = n0 + 32 * quarter + lane;
@@ -488,31 +495,41 @@ __global__ void __launch_bounds__(kTileThreads2) k_linear_tile(const LinearArgs 
             }
         }
     } else {
-        // the cluster's CTAs share the columns out: CTA r gets everybody's sums of columns r * share ..
-        const int share = BT / split, by = __ffs(share) - 1;  // (powers of two)
+        // the cluster's CTAs share the columns out: CTA r gets everybody's sums of columns r * share .., four columns of a channel
+        // in 16 bytes
+        const int share = BT / split, by = __ffs(share) - 1;  // (powers of two, share at least 4)
         cluster_sync();  // every CTA is done with its stages
         if (warp >= 2) {
 #pragma unroll 1
-            for (int c = 0; c < BT; c += 32) {
+            for (int c = 0; c < BT && t0 + c < a.rows; c += 32) {
                 int32_t v[32];
                 tmem_load32(row + c, v);
 #pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    const int to = (c + j) >> by, slot = slice * share + (c + j) - to * share;
-                    const uint32_t at = in_cta(stages + (uint32_t)(slot * kTileRows + 32 * quarter + lane) * 4, (uint32_t)to);
-                    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(v[j]) : "memory");
+                for (int j = 0; j < 32; j += 4) {
+                    const int to = (c + j) >> by, slot = (slice * share + (c + j) - to * share) / 4;
+                    const uint32_t at = in_cta(stages + (uint32_t)(slot * kTileRows + 32 * quarter + lane) * 16, (uint32_t)to);
+                    asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v[j]), "r"(v[j + 1]), "r"(v[j + 2]), "r"(v[j + 3]) : "memory");
                 }
             }
         }
+        const int32_t t1 = t0 + slice * share;
+        const float xs = lane < share && t1 + lane < a.rows ? a.xscale[t1 + lane] : 0.0f;
+        const float xs2 = share > 32 && t1 + 32 + lane < a.rows ? a.xscale[t1 + 32 + lane] : 0.0f;
         cluster_sync();
         if (warp >= 2 && ok) {
-            const int32_t* part = reinterpret_cast<const int32_t*>(base + kSharedHead) + 32 * quarter + lane;
-            for (int c = 0; c < share; ++c) {
-                const int32_t t = t0 + slice * share + c;
-                if (t >= a.rows || n >= a.n) break;
-                int32_t sum = 0;
-                for (int r = 0; r < split; ++r) sum += part[(r * share + c) * kTileRows];
-                store_out<DT>(a.y, (int64_t)t * a.ldy + n, scaled(sum, a.xscale[t], ws, bias));
+            const int4* part = reinterpret_cast<const int4*>(base + kSharedHead) + 32 * quarter + lane;
+            for (int c = 0; c < share && t1 + c < a.rows; c += 4) {
+                int32_t sum[4] = {0, 0, 0, 0};
+#pragma unroll 4
+                for (int r = 0; r < split; ++r) {
+                    const int4 p = part[(r * share + c) / 4 * kTileRows];
+                    sum[0] += p.x, sum[1] += p.y, sum[2] += p.z, sum[3] += p.w;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float scale = __shfl_sync(kFullMask, c + i < 32 ? xs : xs2, (c + i) & 31);
+                    if (t1 + c + i < a.rows && n < a.n) store_out<DT>(a.y, (int64_t)(t1 + c + i) * a.ldy + n, scaled(sum[i], scale, ws, bias));
+                }
             }
         }
     }
@@ -655,11 +672,9 @@ __global__ void __launch_bounds__(kPairThreads)
             const uint32_t side = local & 1;
             const int32_t n = n0 + (int32_t)rank * kTileRows + 32 * quarter + lane;
             const float ws = n < a.n ? a.wscale[n] : 0.0f, bias = a.bias && n < a.n ? a.bias[n] : 0.0f;
-            if (!mbar_wait(&s.done[side], (local >> 1) & 1, gave_up)) lost = true;
-            if (__any_sync(kFullMask, lost)) {
-                lost = true;
-                break;
-            }
+            if (lane == 0 && !mbar_wait(&s.done[side], (local >> 1) & 1, gave_up)) lost = true;
+            lost = __any_sync(kFullMask, lost);
+            if (lost) break;
             mma_fence_after();
             const uint32_t row = tmem + ((uint32_t)(32 * quarter) << 16) + side * BT;
 #pragma unroll 1
@@ -735,11 +750,11 @@ bool launch_pair(const LinearArgs& a, int n_sm, int dev, cudaStream_t st) {
 
 template <int M, int DT>
 bool launch_rows_of(const LinearArgs& a, int n_sm, cudaStream_t st) {
-    // two channels a warp where that still leaves a dozen warps an SM (each then has more loads on their way), and warps that
-    // share a channel where there are too few channels, down to four loads a lane
+    // two channels a warp where that still leaves a dozen warps an SM (each then has more loads on their way); warps share a
+    // channel, down to four loads a lane of each, until there are enough blocks for the SMs to finish together
     const bool two = a.n >= 24 * n_sm;
     int parts = 1;
-    while (parts < kRowsWarps && (int64_t)a.n * parts < 12 * (int64_t)n_sm && a.k >= 4 * 512 * 2 * parts) parts *= 2;
+    while (parts < kRowsWarps && (int64_t)a.n * parts < 6 * (two ? 2 : 1) * kRowsWarps * (int64_t)n_sm && a.k >= 4 * 512 * 2 * parts) parts *= 2;
     const int64_t step = kRowsWarps / parts * (two ? 2 : 1), most = 65535 * (int64_t)M;  // (the grid's second extent)
     for (int64_t t0 = 0; t0 < a.rows; t0 += most) {
         LinearArgs part = a;

@@ -1,0 +1,238 @@
+// Calls on rows in 8 bits straight from torch tensors (module _native).  A single token's norm or product takes the GPU 2 to 5 us;
+// checking its tensors and marshalling 17 arguments in Python takes two to three times that, so it is done here.  Only argument
+// checks and pointers: the calls are those of the C ABI, whose addresses bind() gets from the library that binding.py
+// loaded.
+#define PY_SSIZE_T_CLEAN
+#include <Python.h>
+
+#include <c10/cuda/CUDAFunctions.h>
+#include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/autograd/python_variable.h>
+
+#include "dnns.h"
+
+namespace {
+
+struct Calls {
+    decltype(&dnns_quantize_rows) quantize_rows;
+    decltype(&dnns_rmsnorm_quantize) rmsnorm_quantize;
+    decltype(&dnns_rmsnorm_backward) rmsnorm_backward;
+    decltype(&dnns_silu_gate_quantize) silu_gate_quantize;
+    decltype(&dnns_silu_gate_backward) silu_gate_backward;
+    decltype(&dnns_linear_quantized) linear_quantized;
+} g_calls = {};
+
+// Rows in 8 bits: the addresses of a RowsQ8's tensors, which it keeps alive.
+struct Rows {
+    PyObject_HEAD
+    int8_t* q;
+    float* scale;
+    uint16_t* values;
+    int64_t ldq, ldv, rows, cols;
+};
+PyTypeObject RowsType = {PyVarObject_HEAD_INIT(nullptr, 0)};
+
+struct Matrix {
+    void* p = nullptr;
+    int64_t ld = 0;
+};
+
+bool refuse(const char* what, const char* wants, PyObject* got) {
+    PyErr_Format(PyExc_ValueError, "%s: %s is needed, got %R", what, wants, got);
+    return false;
+}
+
+const at::Tensor* tensor_of(PyObject* o) { return THPVariable_Check(o) ? &THPVariable_Unpack(o) : nullptr; }
+
+bool on_device(const at::Tensor& t, const char* what) {
+    if (t.is_cuda() && t.get_device() == c10::cuda::current_device()) return true;
+    PyErr_Format(PyExc_ValueError, "%s: a tensor of the current CUDA device is needed", what);
+    return false;
+}
+
+// dtype of a matrix of fp32 or bf16
+bool dtype_of(PyObject* o, const char* what, at::ScalarType* type, int32_t* dtype) {
+    const at::Tensor* t = tensor_of(o);
+    if (!t || t->dim() != 2 || (t->scalar_type() != at::kFloat && t->scalar_type() != at::kBFloat16))
+        return refuse(what, "a float32 or bfloat16 matrix", o);
+    *type = t->scalar_type();
+    *dtype = *type == at::kFloat ? DNNS_F32 : DNNS_BF16;
+    return true;
+}
+
+// a rows x cols matrix of unit column stride
+bool matrix(PyObject* o, int64_t rows, int64_t cols, at::ScalarType type, const char* what, Matrix* m) {
+    const at::Tensor* t = tensor_of(o);
+    if (!t || t->dim() != 2 || t->scalar_type() != type || t->size(0) != rows || t->size(1) != cols || (cols > 1 && t->stride(1) != 1)) {
+        PyErr_Format(PyExc_ValueError, "%s: a %lld x %lld matrix of the right type with unit column stride is needed", what, (long long)rows, (long long)cols);
+        return false;
+    }
+    if (!on_device(*t, what)) return false;
+    m->p = t->data_ptr();
+    m->ld = rows > 1 ? t->stride(0) : std::max(cols, t->stride(0));
+    return true;
+}
+bool matrix_or_none(PyObject* o, int64_t rows, int64_t cols, at::ScalarType type, const char* what, Matrix* m) {
+    return o == Py_None || matrix(o, rows, cols, type, what, m);
+}
+
+bool vector_or_none(PyObject* o, int64_t n, const char* what, float** p) {
+    *p = nullptr;
+    if (o == Py_None) return true;
+    const at::Tensor* t = tensor_of(o);
+    if (!t || t->scalar_type() != at::kFloat || t->dim() != 1 || t->size(0) != n || !t->is_contiguous()) {
+        PyErr_Format(PyExc_ValueError, "%s: a contiguous float32 vector of %lld is needed", what, (long long)n);
+        return false;
+    }
+    if (!on_device(*t, what)) return false;
+    *p = static_cast<float*>(t->data_ptr());
+    return true;
+}
+
+Rows* rows_of(PyObject* o) {
+    if (Py_TYPE(o) == &RowsType) return reinterpret_cast<Rows*>(o);
+    refuse("rows", "rows in 8 bits", o);
+    return nullptr;
+}
+
+void* stream() { return c10::cuda::getCurrentCUDAStream().stream(); }
+
+bool count_is(Py_ssize_t n, Py_ssize_t want) {
+    if (n != want) PyErr_Format(PyExc_TypeError, "%zd arguments are needed, got %zd", want, n);
+    return n == want;
+}
+
+PyObject* status(dnns_status s) { return PyLong_FromLong(s); }
+
+// bind(addresses in the order of Calls)
+PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!count_is(n, (Py_ssize_t)(sizeof(Calls) / sizeof(void*)))) return nullptr;
+    void* p[sizeof(Calls) / sizeof(void*)];
+    for (Py_ssize_t i = 0; i < n; ++i)
+        if (!(p[i] = PyLong_AsVoidPtr(a[i]))) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_ValueError, "address %zd is null", i);
+    static_assert(sizeof(p) == sizeof(Calls), "one address a call");
+    memcpy(&g_calls, p, sizeof(p));
+    Py_RETURN_NONE;
+}
+
+// rows(q, ldq, scale, values, ldv, rows, cols): all integers
+PyObject* rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!count_is(n, 7)) return nullptr;
+    long long v[7];
+    for (int i = 0; i < 7; ++i) {
+        v[i] = PyLong_AsLongLong(a[i]);
+        if (v[i] == -1 && PyErr_Occurred()) return nullptr;
+    }
+    Rows* r = PyObject_New(Rows, &RowsType);
+    if (!r) return nullptr;
+    r->q = reinterpret_cast<int8_t*>(v[0]), r->ldq = v[1], r->scale = reinterpret_cast<float*>(v[2]), r->values = reinterpret_cast<uint16_t*>(v[3]);
+    r->ldv = v[4], r->rows = v[5], r->cols = v[6];
+    return reinterpret_cast<PyObject*>(r);
+}
+
+// quantize_rows(x, rows)
+PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    Rows* r;
+    at::ScalarType type;
+    int32_t dtype;
+    Matrix x;
+    if (!count_is(n, 2) || !(r = rows_of(a[1])) || !dtype_of(a[0], "x", &type, &dtype) || !matrix(a[0], r->rows, r->cols, type, "x", &x)) return nullptr;
+    return status(g_calls.quantize_rows(x.p, x.ld, dtype, r->rows, r->cols, r->q, r->ldq, r->scale, r->values, r->ldv, stream()));
+}
+
+// rmsnorm(x, weight, eps, rows, residual, h)
+PyObject* rmsnorm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    Rows* r;
+    at::ScalarType type;
+    int32_t dtype;
+    Matrix x, res, h;
+    float* w;
+    if (!count_is(n, 6) || !(r = rows_of(a[3])) || !dtype_of(a[0], "x", &type, &dtype) || !matrix(a[0], r->rows, r->cols, type, "x", &x) ||
+        !vector_or_none(a[1], r->cols, "weight", &w) || !matrix_or_none(a[4], r->rows, r->cols, type, "residual", &res) ||
+        !matrix_or_none(a[5], r->rows, r->cols, type, "h", &h))
+        return nullptr;
+    const double eps = PyFloat_AsDouble(a[2]);
+    if (eps == -1.0 && PyErr_Occurred()) return nullptr;
+    return status(g_calls.rmsnorm_quantize(x.p, x.ld, res.p, res.ld, w, (float)eps, dtype, r->rows, r->cols, h.p, h.ld, r->q, r->ldq, r->scale, r->values, r->ldv,
+                                           stream()));
+}
+
+// rmsnorm_backward(dy, h, weight, eps, dx, dweight, dh, workspace)
+PyObject* rmsnorm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    at::ScalarType type;
+    int32_t dtype;
+    if (!count_is(n, 8) || !dtype_of(a[1], "h", &type, &dtype)) return nullptr;
+    const int64_t rows = tensor_of(a[1])->size(0), cols = tensor_of(a[1])->size(1);
+    Matrix dy, h, dx, dh;
+    float *w, *dw;
+    if (!matrix(a[0], rows, cols, type, "dy", &dy) || !matrix(a[1], rows, cols, type, "h", &h) || !vector_or_none(a[2], cols, "weight", &w) ||
+        !matrix(a[4], rows, cols, type, "dx", &dx) || !vector_or_none(a[5], cols, "dweight", &dw) || !matrix_or_none(a[6], rows, cols, type, "dh", &dh))
+        return nullptr;
+    void* ws = nullptr;
+    size_t ws_bytes = 0;
+    if (a[7] != Py_None) {
+        const at::Tensor* t = tensor_of(a[7]);
+        if (!t || !t->is_contiguous()) return refuse("workspace", "a contiguous tensor", a[7]), nullptr;
+        if (!on_device(*t, "workspace")) return nullptr;
+        ws = t->data_ptr(), ws_bytes = t->nbytes();
+    }
+    const double eps = PyFloat_AsDouble(a[3]);
+    if (eps == -1.0 && PyErr_Occurred()) return nullptr;
+    return status(g_calls.rmsnorm_backward(dy.p, dy.ld, h.p, h.ld, w, (float)eps, dh.p, dh.ld, dtype, rows, cols, dx.p, dx.ld, dw, ws, ws_bytes, stream()));
+}
+
+// silu_gate(gate, up, rows)
+PyObject* silu_gate(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    Rows* r;
+    at::ScalarType type;
+    int32_t dtype;
+    Matrix g, u;
+    if (!count_is(n, 3) || !(r = rows_of(a[2])) || !dtype_of(a[0], "gate", &type, &dtype) || !matrix(a[0], r->rows, r->cols, type, "gate", &g) ||
+        !matrix(a[1], r->rows, r->cols, type, "up", &u))
+        return nullptr;
+    return status(g_calls.silu_gate_quantize(g.p, g.ld, u.p, u.ld, dtype, r->rows, r->cols, r->q, r->ldq, r->scale, r->values, r->ldv, stream()));
+}
+
+// silu_gate_backward(dy, gate, up, dgate, dup)
+PyObject* silu_gate_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    at::ScalarType type;
+    int32_t dtype;
+    if (!count_is(n, 5) || !dtype_of(a[1], "gate", &type, &dtype)) return nullptr;
+    const int64_t rows = tensor_of(a[1])->size(0), cols = tensor_of(a[1])->size(1);
+    static const char* const names[] = {"dy", "gate", "up", "dgate", "dup"};
+    Matrix m[5];
+    for (int i = 0; i < 5; ++i)
+        if (!matrix(a[i], rows, cols, type, names[i], &m[i])) return nullptr;
+    return status(g_calls.silu_gate_backward(m[0].p, m[0].ld, m[1].p, m[1].ld, m[2].p, m[2].ld, dtype, rows, cols, m[3].p, m[3].ld, m[4].p, m[4].ld, stream()));
+}
+
+// linear(x rows, weight rows, bias or None, y, status address)
+PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    Rows *x, *w;
+    at::ScalarType type;
+    int32_t dtype;
+    Matrix y;
+    float* bias;
+    if (!count_is(n, 5) || !(x = rows_of(a[0])) || !(w = rows_of(a[1])) || !vector_or_none(a[2], w->rows, "bias", &bias) ||
+        !dtype_of(a[3], "y", &type, &dtype) || !matrix(a[3], x->rows, w->rows, type, "y", &y))
+        return nullptr;
+    if (x->cols != w->cols) return PyErr_Format(PyExc_ValueError, "x has %lld columns, the layer %lld", (long long)x->cols, (long long)w->cols);
+    uint32_t* where = static_cast<uint32_t*>(PyLong_AsVoidPtr(a[4]));
+    if (!where && PyErr_Occurred()) return nullptr;
+    return status(g_calls.linear_quantized(x->q, x->ldq, x->scale, w->q, w->ldq, w->scale, bias, x->rows, x->cols, w->rows, dtype, y.p, y.ld, where, stream()));
+}
+
+#define DNNS_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
+PyMethodDef methods[] = {DNNS_METHOD(bind),      DNNS_METHOD(rows),      DNNS_METHOD(quantize_rows),      DNNS_METHOD(rmsnorm), DNNS_METHOD(rmsnorm_backward),
+                         DNNS_METHOD(silu_gate), DNNS_METHOD(silu_gate_backward), DNNS_METHOD(linear), {nullptr, nullptr, 0, nullptr}};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "Calls on rows in 8 bits from torch tensors.", -1, methods};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__native() {
+    RowsType.tp_name = "_native.Rows";
+    RowsType.tp_basicsize = sizeof(Rows);
+    RowsType.tp_flags = Py_TPFLAGS_DEFAULT;
+    if (PyType_Ready(&RowsType) < 0) return nullptr;
+    return PyModule_Create(&module);
+}

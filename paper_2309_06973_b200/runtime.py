@@ -391,28 +391,17 @@ class Deflater:
 
 
 # ---- variants in 8 bits ------------------------------------------------------------------------------------
-_DTYPE = {torch.float32: B.DNNS_F32, torch.bfloat16: B.DNNS_BF16}
+# The calls check their tensors, take the current stream and enter the library in _native (compiled beside it).
+from . import _native  # noqa: E402  (after torch, whose libraries it needs)
+
+_native.bind(*(C.cast(getattr(B.lib(), name), C.c_void_p).value for name in (
+    "dnns_quantize_rows", "dnns_rmsnorm_quantize", "dnns_rmsnorm_backward", "dnns_silu_gate_quantize", "dnns_silu_gate_backward",
+    "dnns_linear_quantized")))
 
 
-def _matrix(t: torch.Tensor, rows: int, cols: int, dtype, what: str):
-    """(address, row stride) of a rows x cols device matrix with unit column stride; raises on anything else."""
-    if t.dtype is not dtype or not t.is_cuda or t.shape != (rows, cols) or (cols > 1 and t.stride(1) != 1):
-        raise ValueError(f"{what}: a {rows} x {cols} {dtype} CUDA matrix with unit column stride is needed, "
-                         f"got {tuple(t.shape)} {t.dtype} strides {t.stride()} on {t.device}")
-    return t.data_ptr(), t.stride(0) if rows > 1 else max(cols, t.stride(0))
-
-
-def _vector(t: torch.Tensor, n: int, what: str) -> int:
-    if t.dtype is not torch.float32 or not t.is_cuda or t.shape != (n,) or not t.is_contiguous():
-        raise ValueError(f"{what}: a contiguous float32 CUDA vector of {n} is needed, got {tuple(t.shape)} {t.dtype}")
-    return t.data_ptr()
-
-
-def _dtype_of(t: torch.Tensor, what: str) -> int:
-    d = _DTYPE.get(t.dtype)
-    if d is None or t.dim() != 2:
-        raise ValueError(f"{what}: a float32 or bfloat16 matrix is needed, got {t.dim()} dimensions of {t.dtype}")
-    return d
+def _done(status: int, where: str):
+    if status:
+        raise B.DnnsError(status, where)
 
 
 class RowsQ8:
@@ -432,32 +421,30 @@ class RowsQ8:
         return self
 
     def _set(self, q, scale, cols, values):
+        rows = q.shape[0]
         if q.dtype is not torch.int8 or q.dim() != 2 or not q.is_cuda or q.shape[1] < cols or (q.shape[1] > 1 and q.stride(1) != 1):
             raise ValueError(f"q: an int8 CUDA matrix of at least {cols} columns is needed, got {tuple(q.shape)} {q.dtype}")
-        self.rows, self.cols, self.q, self.scale, self.values = q.shape[0], cols, q, scale, values
-        self.device = q.device
-        self.q_ptr, self.ld = q.data_ptr(), q.stride(0) if self.rows > 1 else B.dnns_quantized_row_bytes(cols)
-        self.scale_ptr = _vector(scale, self.rows, "scale")
-        self.values_ptr, self.ldv = (0, 0) if values is None else _matrix(values, self.rows, cols, torch.bfloat16, "values")
+        if scale.dtype is not torch.float32 or scale.shape != (rows,) or not scale.is_contiguous() or scale.device != q.device:
+            raise ValueError(f"scale: a contiguous float32 vector of {rows} beside q is needed, got {tuple(scale.shape)} {scale.dtype}")
+        if values is not None and (values.dtype is not torch.bfloat16 or values.shape != (rows, cols) or values.device != q.device
+                                   or (cols > 1 and values.stride(1) != 1)):
+            raise ValueError(f"values: a {rows} x {cols} bfloat16 matrix beside q is needed, got {tuple(values.shape)} {values.dtype}")
+        self.rows, self.cols, self.q, self.scale, self.values, self.device = rows, cols, q, scale, values, q.device
+        self._c = _native.rows(q.data_ptr(), q.stride(0) if rows > 1 else B.dnns_quantized_row_bytes(cols), scale.data_ptr(),
+                               0 if values is None else values.data_ptr(),
+                               0 if values is None else values.stride(0) if rows > 1 else cols, rows, cols)
 
 
 def quantize_rows(x: torch.Tensor, out: RowsQ8) -> RowsQ8:
     """The rows of x in 8 bits: a weight matrix per output channel, or an activation per token."""
-    dtype = _dtype_of(x, "x")
-    p, ld = _matrix(x, out.rows, out.cols, x.dtype, "x")
-    B.dnns_quantize_rows(p, ld, dtype, out.rows, out.cols, out.q_ptr, out.ld, out.scale_ptr, out.values_ptr, out.ldv, _stream())
+    _done(_native.quantize_rows(x, out._c), "dnns_quantize_rows")
     return out
 
 
 def rmsnorm_q8(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float, out: RowsQ8,
                residual: Optional[torch.Tensor] = None, h: Optional[torch.Tensor] = None) -> RowsQ8:
     """h = x + residual (stored when given; may be x or residual), out = h * weight / sqrt(mean(h^2) + eps) in 8 bits."""
-    dtype, rows, cols = _dtype_of(x, "x"), out.rows, out.cols
-    p, ld = _matrix(x, rows, cols, x.dtype, "x")
-    pr, ldr = (0, 0) if residual is None else _matrix(residual, rows, cols, x.dtype, "residual")
-    ph, ldh = (0, 0) if h is None else _matrix(h, rows, cols, x.dtype, "h")
-    B.dnns_rmsnorm_quantize(p, ld, pr, ldr, 0 if weight is None else _vector(weight, cols, "weight"), eps, dtype, rows, cols, ph, ldh,
-                            out.q_ptr, out.ld, out.scale_ptr, out.values_ptr, out.ldv, _stream())
+    _done(_native.rmsnorm(x, weight, eps, out._c, residual, h), "dnns_rmsnorm_quantize")
     return out
 
 
@@ -470,55 +457,35 @@ def rmsnorm_q8_backward(dy: torch.Tensor, h: torch.Tensor, weight: Optional[torc
                         workspace: Optional[torch.Tensor] = None) -> None:
     """The norm's gradient at h: dx (of x and residual alike; dh, the gradient that reaches h past the norm, added) and
     dweight, which needs a workspace."""
-    dtype, (rows, cols) = _dtype_of(h, "h"), h.shape
-    m = lambda t, what: (0, 0) if t is None else _matrix(t, rows, cols, h.dtype, what)
-    pdy, lddy = m(dy, "dy")
-    ph, ldh = m(h, "h")
-    pdh, lddh = m(dh, "dh")
-    pdx, lddx = m(dx, "dx")
-    B.dnns_rmsnorm_backward(pdy, lddy, ph, ldh, 0 if weight is None else _vector(weight, cols, "weight"), eps, pdh, lddh, dtype,
-                            rows, cols, pdx, lddx, 0 if dweight is None else _vector(dweight, cols, "dweight"),
-                            0 if workspace is None else workspace.data_ptr(),
-                            0 if workspace is None else workspace.numel() * workspace.element_size(), _stream())
+    _done(_native.rmsnorm_backward(dy, h, weight, eps, dx, dweight, dh, workspace), "dnns_rmsnorm_backward")
 
 
 def silu_gate_q8(gate: torch.Tensor, up: torch.Tensor, out: RowsQ8) -> RowsQ8:
     """out = silu(gate) * up in 8 bits."""
-    dtype = _dtype_of(gate, "gate")
-    pg, ldg = _matrix(gate, out.rows, out.cols, gate.dtype, "gate")
-    pu, ldu = _matrix(up, out.rows, out.cols, gate.dtype, "up")
-    B.dnns_silu_gate_quantize(pg, ldg, pu, ldu, dtype, out.rows, out.cols, out.q_ptr, out.ld, out.scale_ptr, out.values_ptr,
-                              out.ldv, _stream())
+    _done(_native.silu_gate(gate, up, out._c), "dnns_silu_gate_quantize")
     return out
 
 
 def silu_gate_q8_backward(dy: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, dgate: torch.Tensor, dup: torch.Tensor) -> None:
     """Gradients of gate and up."""
-    dtype, (rows, cols) = _dtype_of(gate, "gate"), gate.shape
-    a = []
-    for t, what in ((dy, "dy"), (gate, "gate"), (up, "up"), (dgate, "dgate"), (dup, "dup")):
-        a.append(_matrix(t, rows, cols, gate.dtype, what))
-    B.dnns_silu_gate_backward(*a[0], *a[1], *a[2], dtype, rows, cols, *a[3], *a[4], _stream())
+    _done(_native.silu_gate_backward(dy, gate, up, dgate, dup), "dnns_silu_gate_backward")
 
 
 class LinearQ8:
     """A layer whose weights are rows in 8 bits (a scale per output channel), applied to tokens in 8 bits."""
 
     def __init__(self, weight: RowsQ8, bias: Optional[torch.Tensor] = None):
+        if bias is not None and (bias.dtype is not torch.float32 or bias.shape != (weight.rows,) or not bias.is_contiguous()
+                                 or bias.device != weight.device):
+            raise ValueError(f"bias: a contiguous float32 vector of {weight.rows} beside the weights is needed, "
+                             f"got {tuple(bias.shape)} {bias.dtype}")
         self.weight, self.bias = weight, bias
-        self.bias_ptr = 0 if bias is None else _vector(bias, weight.rows, "bias")
         self.status = torch.zeros(1, dtype=torch.int32, device=weight.device)
-        self._status_ptr = self.status.data_ptr()
+        self._w, self._status_ptr = weight._c, self.status.data_ptr()
 
     def __call__(self, x: RowsQ8, y: torch.Tensor) -> torch.Tensor:
         """y (x.rows, weight.rows) of float32 or bfloat16 = x . weight^T + bias."""
-        w = self.weight
-        if x.cols != w.cols:
-            raise ValueError(f"x has {x.cols} columns, the layer {w.cols}")
-        dtype = _dtype_of(y, "y")
-        p, ld = _matrix(y, x.rows, w.rows, y.dtype, "y")
-        B.dnns_linear_quantized(x.q_ptr, x.ld, x.scale_ptr, w.q_ptr, w.ld, w.scale_ptr, self.bias_ptr, x.rows, x.cols, w.rows,
-                                dtype, p, ld, self._status_ptr, _stream())
+        _done(_native.linear(x._c, self._w, self.bias, y, self._status_ptr), "dnns_linear_quantized")
         return y
 
     def device_status(self) -> int:

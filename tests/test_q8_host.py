@@ -84,5 +84,24 @@ def test_sizes():
     assert B.dnns_rmsnorm_backward_workspace_bytes(0, 64) == 0 == B.dnns_rmsnorm_backward_workspace_bytes(4, 0)
     assert B.dnns_rmsnorm_backward_workspace_bytes(-1, 64) == 0
     a, b = B.dnns_rmsnorm_backward_workspace_bytes(4, 64), B.dnns_rmsnorm_backward_workspace_bytes(1 << 20, 64)
-    assert 4 * 64 * 4 <= a < b <= 1 << 20
+    assert 64 * 4 <= a < b <= 1 << 20                          # at least one slice of partial sums
     assert B.DNNS_LINEAR_MAX_IN * 128 * 128 < 2 ** 31          # what an int32 sum holds
+
+
+def test_native_calls_refuse_what_is_not_on_the_device():
+    """The calls from torch tensors check them before they enter the library."""
+    import torch
+
+    from paper_2309_06973_b200 import runtime as R
+    rows = R._native.rows(A, 16, A, 0, 0, 2, 3)
+    x = torch.zeros(2, 3)
+    for call in (lambda: R._native.quantize_rows(x, rows), lambda: R._native.rmsnorm(x, None, 1e-5, rows, None, None),
+                 lambda: R._native.silu_gate(x, x, rows), lambda: R._native.rmsnorm_backward(x, x, None, 1e-5, x, None, None, None),
+                 lambda: R._native.silu_gate_backward(x, x, x, x, x), lambda: R._native.linear(rows, R._native.rows(A, 16, A, 0, 0, 3, 3), None, x, A),
+                 lambda: R._native.quantize_rows(x.t(), rows), lambda: R._native.quantize_rows(x.half(), rows),
+                 lambda: R._native.quantize_rows("x", rows), lambda: R._native.quantize_rows(x, x), lambda: R.RowsQ8.of(x.to(torch.int8), x[:, 0], 3)):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: R._native.quantize_rows(x), lambda: R._native.rows(1, 2), lambda: R._native.bind(1)):
+        with pytest.raises(TypeError):
+            call()
