@@ -2,11 +2,12 @@
 // The sum is exact in int32 (at most 2^17 - 1 products of at most 2^14 each), so any order and any split of it gives
 // the same bits.
 //
-// Three kernels, chosen by the number of tokens and the work there is for the SMs (choose() below):
-//   k_linear_rows   few tokens: bound by reading the weights once; int8 dot products in the ordinary pipes
-//   k_linear_tile   one CTA a tile of 128 channels x BT tokens; the columns of a tile may be split over the CTAs of a cluster,
-//                   whose int32 partial sums meet in distributed shared memory
-//   k_linear_pair   two CTAs a tile of 256 channels x BT tokens, persistent, accumulators double-buffered in tensor memory
+// Four kernels, chosen by the number of tokens and the work there is for the SMs (choose() below):
+//   k_linear_rows   one token: bound by reading the weights once; int8 dot products in the ordinary pipes
+//   k_linear_few    up to 32 tokens: the same, with warp-wide products
+//   k_linear_tile   one CTA a tile of 128 channels by up to 256 tokens; the columns of a tile may be split over the CTAs of a
+//                   cluster, whose int32 partial sums meet in distributed shared memory
+//   k_linear_pair   two CTAs a tile of 256 channels by up to 256 tokens, persistent, accumulators double-buffered in tensor memory
 // The tile kernels put the WEIGHTS on the rows of the tensor cores' tile (the lanes of tensor memory) and the tokens on its
 // columns: a tile is then never wider in tokens than there are tokens to a multiple of 32, and a warp that reads one
 // accumulator column holds 32 neighbouring channels of one token, which it stores as one contiguous piece of y - no
@@ -14,6 +15,7 @@
 #include <cuda.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "dnns_internal.cuh"
 
@@ -352,14 +354,13 @@ __device__ __forceinline__ void tmem_load32(uint32_t at, int32_t (&v)[32]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
-// 32 columns (tokens t0 ..) of one channel a lane: scale and store.
+// Up to 32 columns (tokens t0 .. t0 + left - 1) of one channel a lane: scale and store.
 template <int DT>
-__device__ __forceinline__ void store_columns(const LinearArgs& a, const int32_t (&v)[32], int32_t t0, int32_t n, float ws, float bias) {
+__device__ __forceinline__ void store_columns(const LinearArgs& a, const int32_t (&v)[32], int32_t t0, int32_t left, int32_t n, float ws, float bias) {
     typedef typename std::conditional<DT == DNNS_F32, float, uint16_t>::type T;
     const int lane = threadIdx.x & 31;
-    const float mine = t0 + lane < a.rows ? a.xscale[t0 + lane] : 0.0f;
+    const float mine = lane < left ? a.xscale[t0 + lane] : 0.0f;
     T* y = static_cast<T*>(a.y) + (int64_t)t0 * a.ldy + n;
-    const int32_t left = a.rows - t0;
     const bool in = n < a.n;
 #pragma unroll
     for (int j = 0; j < 32; ++j) {
@@ -369,8 +370,9 @@ __device__ __forceinline__ void store_columns(const LinearArgs& a, const int32_t
     }
 }
 
+constexpr int kMaxStages = 10;
 struct TileShared {  // in front of the stages
-    uint64_t full[10], empty[10], done[2], taken[2], drain;
+    uint64_t full[kMaxStages], empty[kMaxStages], done[2], taken[2], drain;
     uint32_t tmem, gave_up;
 };
 constexpr uint32_t kSharedHead = 1024;
@@ -384,33 +386,30 @@ __device__ __forceinline__ unsigned char* shared_base() {
 // ================= one CTA a tile, its columns split over a cluster =================
 constexpr int kTileThreads2 = 192;  // warp 0 loads, warp 1 issues the products, warps 2 .. 5 read the accumulators
 
-template <int BT>
-struct TileCfg {
-    static constexpr uint32_t kStage = kWeightBytes + BT * kBlockK;
-    #ifndef ST32
-#define ST32 5
-#endif
-    static constexpr int kStages = BT <= 32 ? ST32 : BT <= 64 ? 4 : 6;
-    static constexpr uint32_t kShared = kSharedHead + kStages * kStage + 1024;
-    static constexpr uint32_t kColumns = BT;
-    static_assert(kStages <= 10 && kStages * kStage >= BT * kTileRows * 4, "the partial sums of a cluster reuse the stages");
+// How a product is cut: tiles of `tokens` (a multiple of 32 up to 256), each over `split` CTAs of a cluster; a share of the
+// tokens, tokens / split, is a multiple of 4.
+struct TilePlan {
+    int32_t tokens, t_tiles, split, stages;
+    __host__ __device__ uint32_t stage_bytes() const { return kWeightBytes + (uint32_t)tokens * kBlockK; }
+    // the stages, then (split) the partial sums that the other CTAs send
+    __host__ __device__ uint32_t sums_at() const { return kSharedHead + (uint32_t)stages * stage_bytes(); }
+    uint32_t shared_bytes() const { return sums_at() + (split > 1 ? (uint32_t)tokens * kTileRows * 4 : 0) + 1024; }
 };
-
-template <int BT, int DT>
+template <int DT>
 __global__ void __launch_bounds__(kTileThreads2) k_linear_tile(const LinearArgs a, const __grid_constant__ CUtensorMap wmap,
-                                                               const __grid_constant__ CUtensorMap xmap, int32_t t_tiles, int32_t split) {
-    typedef TileCfg<BT> Cfg;
+                                                               const __grid_constant__ CUtensorMap xmap, const TilePlan plan) {
     unsigned char* base = shared_base();
     TileShared& s = *reinterpret_cast<TileShared*>(base);
-    const uint32_t stages = smem_addr(base) + kSharedHead;
+    const uint32_t stages = smem_addr(base) + kSharedHead, stage_bytes = plan.stage_bytes();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int32_t tile = blockIdx.x / split, slice = blockIdx.x - tile * split;
-    const int32_t t0 = (tile % t_tiles) * BT, n0 = (tile / t_tiles) * kTileRows;
+    const int32_t split = plan.split, tile = blockIdx.x / split, slice = blockIdx.x - tile * split;
+    const int32_t t_tile = tile % plan.t_tiles, t0 = t_tile * plan.tokens, n0 = tile / plan.t_tiles * kTileRows;
     const int32_t blocks = (a.k + kBlockK - 1) / kBlockK;
     const int32_t kb0 = (int32_t)((int64_t)blocks * slice / split), kbs = (int32_t)((int64_t)blocks * (slice + 1) / split) - kb0;
+    const uint32_t columns = plan.tokens <= 32 ? 32 : plan.tokens <= 64 ? 64 : plan.tokens <= 128 ? 128 : 256;  // of tensor memory
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < Cfg::kStages; ++i) mbar_init(&s.full[i], 1), mbar_init(&s.empty[i], 1);
+        for (int i = 0; i < plan.stages; ++i) mbar_init(&s.full[i], 1), mbar_init(&s.empty[i], 1);
         mbar_init(&s.done[0], 1);
         mbar_init(&s.drain, 1);
         s.gave_up = 0;
@@ -420,11 +419,13 @@ __global__ void __launch_bounds__(kTileThreads2) k_linear_tile(const LinearArgs 
     }
     if (warp == 1) {
         __syncwarp();
-        tmem_alloc<false>(&s.tmem, Cfg::kColumns);
+        tmem_alloc<false>(&s.tmem, columns);
         mma_fence_before();
     }
     __syncthreads();
     mma_fence_after();
+    // (the cluster's CTAs are all there before one of them sends its sums to another: waited for below)
+    if (split > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     chain_go();  // (not before this CTA has its tensor memory: the next kernel's CTAs would take it and wait for this one's end)
     chain_wait();
     const uint32_t tmem = s.tmem;
@@ -432,36 +433,39 @@ __global__ void __launch_bounds__(kTileThreads2) k_linear_tile(const LinearArgs 
 
     if (warp == 0) {
         if (lane == 0) {
-            int32_t it = 0;
+            int32_t it = 0, st = 0;
+            uint32_t turn = 1;
             for (; it < kbs; ++it) {
-                const int st = it % Cfg::kStages;
-                if (!mbar_wait(&s.empty[st], ((it / Cfg::kStages) & 1) ^ 1, gave_up)) break;
-                const uint32_t at = stages + st * Cfg::kStage, bar = smem_addr(&s.full[st]);
-                mbar_expect(&s.full[st], Cfg::kStage);
+                if (!mbar_wait(&s.empty[st], turn, gave_up)) break;
+                const uint32_t at = stages + st * stage_bytes, bar = smem_addr(&s.full[st]);
+                mbar_expect(&s.full[st], stage_bytes);
                 tile_load<false>(at, &wmap, (kb0 + it) * kBlockK, n0, bar);
                 tile_load<false>(at + kWeightBytes, &xmap, (kb0 + it) * kBlockK, t0, bar);
+                if (++st == plan.stages) st = 0, turn ^= 1;
             }
             // a wait that was given up: copies in flight are waited for (again with a limit) before the memory is left
             if (it < kbs) {
                 atomicCAS(a.status, 0u, (uint32_t)DNNS_ERR_TIMEOUT);
                 const uint64_t since = global_ns();
-                for (int32_t u = max(0, it - Cfg::kStages); u < it; ++u)
-                    while (!mbar_try(&s.full[u % Cfg::kStages], (u / Cfg::kStages) & 1) && global_ns() - since < kWaitLimitNs) {
+                for (int32_t u = max(0, it - plan.stages); u < it; ++u)
+                    while (!mbar_try(&s.full[u % plan.stages], (u / plan.stages) & 1) && global_ns() - since < kWaitLimitNs) {
                     }
             }
         }
     } else if (warp == 1) {
         if (lane == 0) {
-            int32_t it = 0;
+            const uint32_t shape = mma_shape(kTileRows, plan.tokens);
+            int32_t it = 0, st = 0;
+            uint32_t turn = 0;
             for (; it < kbs; ++it) {
-                const int st = it % Cfg::kStages;
-                if (!mbar_wait(&s.full[st], (it / Cfg::kStages) & 1, gave_up)) break;
+                if (!mbar_wait(&s.full[st], turn, gave_up)) break;
                 mma_fence_after();
-                const uint32_t at = stages + st * Cfg::kStage;
+                const uint32_t at = stages + st * stage_bytes;
                 const uint64_t w = operand(at), x = operand(at + kWeightBytes);
 #pragma unroll
-                for (int q = 0; q < kBlockK / 32; ++q) mma<false>(tmem, w + 2 * q, x + 2 * q, mma_shape(kTileRows, BT), it > 0 || q > 0);
+                for (int q = 0; q < kBlockK / 32; ++q) mma<false>(tmem, w + 2 * q, x + 2 * q, shape, it > 0 || q > 0);
                 mma_commit<false>(&s.empty[st]);
+                if (++st == plan.stages) st = 0, turn ^= 1;
             }
             if (it == kbs) {
                 mma_commit<false>(&s.done[0]);
@@ -474,62 +478,71 @@ __global__ void __launch_bounds__(kTileThreads2) k_linear_tile(const LinearArgs 
             }
         }
     }
+    const int quarter = warp & 3;  // tensor memory lanes a warp may read: 32 * (its index mod 4) ..
+    const int32_t n = n0 + 32 * quarter + lane;
+    const float ws = warp >= 2 && n < a.n ? a.wscale[n] : 0.0f, bias = warp >= 2 && a.bias && n < a.n ? a.bias[n] : 0.0f;
     // everybody waits for the sums: after this no copy and no product of this CTA is in flight
     __syncwarp();
     const bool ok = __shfl_sync(kFullMask, (int)(lane == 0 && mbar_wait(&s.done[0], 0, gave_up)), 0);
     mma_fence_after();
-    const int quarter = warp & 3;  // tensor memory lanes a warp may read: 32 * (its index mod 4) ..
-    const int32_t n = n0 + 32 * quarter + lane;
-    const float ws = warp >= 2 && n < a.n ? a.wscale[n] : 0.0f, bias = warp >= 2 && a.bias && n < a.n ? a.bias[n] : 0.0f;
     const uint32_t row = tmem + ((uint32_t)(32 * quarter) << 16);
     if (!ok && threadIdx.x == 64) atomicCAS(a.status, 0u, (uint32_t)DNNS_ERR_TIMEOUT);
     __syncwarp();
     if (split == 1) {
         if (warp >= 2 && ok) {
 #pragma unroll 1
-            for (int c = 0; c < BT; c += 32) {
-                if (t0 + c >= a.rows) break;
+            for (int c = 0; c < plan.tokens && t0 + c < a.rows; c += 32) {
                 int32_t v[32];
                 tmem_load32(row + c, v);
-                store_columns<DT>(a, v, t0 + c, n, ws, bias);
+                store_columns<DT>(a, v, t0 + c, a.rows - t0 - c, n, ws, bias);
             }
         }
     } else {
         // the cluster's CTAs share the columns out: CTA r gets everybody's sums of columns r * share .., four columns of a channel
         // in 16 bytes
-        const int share = BT / split, by = __ffs(share) - 1;  // (powers of two, share at least 4)
-        cluster_sync();  // every CTA is done with its stages
+        const int share = plan.tokens / split;
+        const uint32_t sums = smem_addr(base) + plan.sums_at();
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // (the barrier arrived at above)
         if (warp >= 2) {
+            int to = 0, slot = slice * (share / 4);  // of the next four columns: the CTA they go to, and their place there
+            uint32_t dest = in_cta(sums, 0);
 #pragma unroll 1
-            for (int c = 0; c < BT && t0 + c < a.rows; c += 32) {
+            for (int c = 0; c < plan.tokens && t0 + c < a.rows; c += 32) {
                 int32_t v[32];
                 tmem_load32(row + c, v);
 #pragma unroll
                 for (int j = 0; j < 32; j += 4) {
-                    const int to = (c + j) >> by, slot = (slice * share + (c + j) - to * share) / 4;
-                    const uint32_t at = in_cta(stages + (uint32_t)(slot * kTileRows + 32 * quarter + lane) * 16, (uint32_t)to);
-                    asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v[j]), "r"(v[j + 1]), "r"(v[j + 2]), "r"(v[j + 3]) : "memory");
+                    asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dest + (uint32_t)(slot * kTileRows + 32 * quarter + lane) * 16), "r"(v[j]),
+                                 "r"(v[j + 1]), "r"(v[j + 2]), "r"(v[j + 3])
+                                 : "memory");
+                    if (++slot == (slice + 1) * (share / 4)) {
+                        slot = slice * (share / 4);
+                        ++to;
+                        dest = in_cta(sums, (uint32_t)min(to, split - 1));
+                    }
                 }
             }
         }
-        const int32_t t1 = t0 + slice * share;
-        const float xs = lane < share && t1 + lane < a.rows ? a.xscale[t1 + lane] : 0.0f;
-        const float xs2 = share > 32 && t1 + 32 + lane < a.rows ? a.xscale[t1 + 32 + lane] : 0.0f;
         cluster_sync();
         if (warp >= 2 && ok) {
-            const int4* part = reinterpret_cast<const int4*>(base + kSharedHead) + 32 * quarter + lane;
-            for (int c = 0; c < share && t1 + c < a.rows; c += 4) {
-                int32_t sum[4] = {0, 0, 0, 0};
-#pragma unroll 4
-                for (int r = 0; r < split; ++r) {
-                    const int4 p = part[(r * share + c) / 4 * kTileRows];
-                    sum[0] += p.x, sum[1] += p.y, sum[2] += p.z, sum[3] += p.w;
-                }
+            const int4* part = reinterpret_cast<const int4*>(base + plan.sums_at()) + 32 * quarter + lane;
+            const int32_t t1 = t0 + slice * share, have = min(share, a.rows - t1);
+#pragma unroll 1
+            for (int c = 0; c < have; c += 32) {
+                int32_t v[32];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float scale = __shfl_sync(kFullMask, c + i < 32 ? xs : xs2, (c + i) & 31);
-                    if (t1 + c + i < a.rows && n < a.n) store_out<DT>(a.y, (int64_t)(t1 + c + i) * a.ldy + n, scaled(sum[i], scale, ws, bias));
+                for (int j = 0; j < 32; ++j) v[j] = 0;
+#pragma unroll 1
+                for (int r = 0; r < split; ++r) {
+                    const int4* from = part + (r * share + c) / 4 * kTileRows;
+#pragma unroll
+                    for (int j = 0; j < 32; j += 4) {
+                        if (c + j >= have) break;
+                        const int4 p = from[j / 4 * kTileRows];
+                        v[j] += p.x, v[j + 1] += p.y, v[j + 2] += p.z, v[j + 3] += p.w;
+                    }
                 }
+                store_columns<DT>(a, v, t1 + c, have - c, n, ws, bias);
             }
         }
     }
@@ -538,7 +551,7 @@ __global__ void __launch_bounds__(kTileThreads2) k_linear_tile(const LinearArgs 
     __syncthreads();
     if (warp == 1) {
         mma_fence_after();
-        tmem_free<false>(tmem, Cfg::kColumns);
+        tmem_free<false>(tmem, columns);
     }
 }
 
@@ -547,25 +560,19 @@ constexpr int kPairThreads = 320;  // warp 0 loads, warp 1 issues the products, 
 constexpr int kPairReaders = 8;
 constexpr int kRaster = 8;         // channel tiles that are walked together, so that what runs at a time shares its operands in L2
 
-template <int BT>
-struct PairCfg {
-    static constexpr uint32_t kTokenBytes = BT / 2 * kBlockK;  // a CTA holds half of the tile's tokens
-    static constexpr uint32_t kStage = kWeightBytes + kTokenBytes;
-    static constexpr int kStages = BT == 256 ? 6 : 8;
-    static constexpr uint32_t kShared = kSharedHead + kStages * kStage + 1024;
-    static constexpr uint32_t kColumns = 2 * BT;
-};
+constexpr uint32_t kPairColumns = 512;  // of tensor memory: two sets of accumulators
 
-template <int BT, int DT>
+template <int DT>
 __global__ void __launch_bounds__(kPairThreads)
-    k_linear_pair(const LinearArgs a, const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap) {
-    typedef PairCfg<BT> Cfg;
+    k_linear_pair(const LinearArgs a, const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, int32_t tokens, int32_t n_stages) {
+    // a CTA holds its 128 channels and half of the tile's tokens
+    const uint32_t stage_bytes = kWeightBytes + (uint32_t)tokens / 2 * kBlockK;
     unsigned char* base = shared_base();
     TileShared& s = *reinterpret_cast<TileShared*>(base);
     const uint32_t stages = smem_addr(base) + kSharedHead;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint32_t rank = cluster_rank();
-    const int32_t n_tiles = (a.n + 2 * kTileRows - 1) / (2 * kTileRows), t_tiles = (a.rows + BT - 1) / BT;
+    const int32_t n_tiles = (a.n + 2 * kTileRows - 1) / (2 * kTileRows), t_tiles = (a.rows + tokens - 1) / tokens;
     const int64_t tiles = (int64_t)n_tiles * t_tiles;
     const int32_t blocks = (a.k + kBlockK - 1) / kBlockK;
     const int64_t first = blockIdx.x >> 1, step = gridDim.x >> 1;
@@ -575,11 +582,11 @@ __global__ void __launch_bounds__(kPairThreads)
         const int32_t wide = min(kRaster, n_tiles - (int32_t)group * kRaster);
         const int32_t t = (int32_t)(in / wide);
         n0 = ((int32_t)group * kRaster + (int32_t)(in - (int64_t)t * wide)) * 2 * kTileRows;
-        t0 = t * BT;
+        t0 = t * tokens;
     };
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < Cfg::kStages; ++i) mbar_init(&s.full[i], 1), mbar_init(&s.empty[i], 1);
+        for (int i = 0; i < n_stages; ++i) mbar_init(&s.full[i], 1), mbar_init(&s.empty[i], 1);
         for (int i = 0; i < 2; ++i) mbar_init(&s.done[i], 1), mbar_init(&s.taken[i], 2 * kPairReaders);
         mbar_init(&s.drain, 1);
         s.gave_up = 0;
@@ -589,7 +596,7 @@ __global__ void __launch_bounds__(kPairThreads)
     }
     if (warp == 1) {
         __syncwarp();
-        tmem_alloc<true>(&s.tmem, Cfg::kColumns);
+        tmem_alloc<true>(&s.tmem, kPairColumns);
         mma_fence_before();
     }
     __syncthreads();
@@ -603,37 +610,38 @@ __global__ void __launch_bounds__(kPairThreads)
 
     if (warp == 0) {
         if (lane == 0) {
-            uint32_t it = 0;
+            uint32_t it = 0, st = 0, turn = 1;
             for (int64_t tile = first; tile < tiles && !lost; tile += step) {
                 int32_t n0, t0;
                 place(tile, n0, t0);
                 for (int32_t kb = 0; kb < blocks; ++kb, ++it) {
-                    const uint32_t st = it % Cfg::kStages;
-                    if (!mbar_wait(&s.empty[st], ((it / Cfg::kStages) & 1) ^ 1, gave_up)) {
+                    if (!mbar_wait(&s.empty[st], turn, gave_up)) {
                         lost = true;
                         break;
                     }
-                    const uint32_t at = stages + st * Cfg::kStage, bar = in_cta(smem_addr(&s.full[st]), 0);
-                    if (rank == 0) mbar_expect(&s.full[st], 2 * Cfg::kStage);
+                    const uint32_t at = stages + st * stage_bytes, bar = in_cta(smem_addr(&s.full[st]), 0);
+                    if (rank == 0) mbar_expect(&s.full[st], 2 * stage_bytes);
                     tile_load<true>(at, &wmap, kb * kBlockK, n0 + (int32_t)rank * kTileRows, bar);
-                    tile_load<true>(at + kWeightBytes, &xmap, kb * kBlockK, t0 + (int32_t)rank * (BT / 2), bar);
+                    tile_load<true>(at + kWeightBytes, &xmap, kb * kBlockK, t0 + (int32_t)rank * (tokens / 2), bar);
+                    if (++st == (uint32_t)n_stages) st = 0, turn ^= 1;
                 }
             }
             // the products that read this CTA's stages are done once their stages are free again; after a wait that was
             // given up, copies in flight are waited for (again with a limit)
-            const uint32_t n = min(it, (uint32_t)Cfg::kStages);
+            const uint32_t n = min(it, (uint32_t)n_stages);
             if (!lost) {
-                for (uint32_t u = it - n; u < it && !lost; ++u) lost = !mbar_wait(&s.empty[u % Cfg::kStages], (u / Cfg::kStages) & 1, gave_up);
+                for (uint32_t u = it - n; u < it && !lost; ++u) lost = !mbar_wait(&s.empty[u % n_stages], (u / n_stages) & 1, gave_up);
             } else if (rank == 0) {
                 const uint64_t since = global_ns();
                 for (uint32_t u = it - n; u < it; ++u)
-                    while (!mbar_try(&s.full[u % Cfg::kStages], (u / Cfg::kStages) & 1) && global_ns() - since < kWaitLimitNs) {
+                    while (!mbar_try(&s.full[u % n_stages], (u / n_stages) & 1) && global_ns() - since < kWaitLimitNs) {
                     }
             }
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
-            uint32_t it = 0, local = 0;
+            const uint32_t shape = mma_shape(2 * kTileRows, tokens);
+            uint32_t st = 0, turn = 0, local = 0;
             for (int64_t tile = first; tile < tiles && !lost; tile += step, ++local) {
                 const uint32_t side = local & 1;
                 if (!mbar_wait(&s.taken[side], ((local >> 1) & 1) ^ 1, gave_up)) {
@@ -641,18 +649,18 @@ __global__ void __launch_bounds__(kPairThreads)
                     break;
                 }
                 mma_fence_after();
-                for (int32_t kb = 0; kb < blocks; ++kb, ++it) {
-                    const uint32_t st = it % Cfg::kStages;
-                    if (!mbar_wait(&s.full[st], (it / Cfg::kStages) & 1, gave_up)) {
+                for (int32_t kb = 0; kb < blocks; ++kb) {
+                    if (!mbar_wait(&s.full[st], turn, gave_up)) {
                         lost = true;
                         break;
                     }
                     mma_fence_after();
-                    const uint32_t at = stages + st * Cfg::kStage;
+                    const uint32_t at = stages + st * stage_bytes;
                     const uint64_t w = operand(at), x = operand(at + kWeightBytes);
 #pragma unroll
-                    for (int q = 0; q < kBlockK / 32; ++q) mma<true>(tmem + side * BT, w + 2 * q, x + 2 * q, mma_shape(2 * kTileRows, BT), kb > 0 || q > 0);
+                    for (int q = 0; q < kBlockK / 32; ++q) mma<true>(tmem + side * 256, w + 2 * q, x + 2 * q, shape, kb > 0 || q > 0);
                     mma_commit<true>(&s.empty[st]);
+                    if (++st == (uint32_t)n_stages) st = 0, turn ^= 1;
                 }
                 if (!lost) mma_commit<true>(&s.done[side]);
             }
@@ -664,7 +672,7 @@ __global__ void __launch_bounds__(kPairThreads)
             }
         }
     } else {
-        const int quarter = warp & 3, half = (warp - 2) >> 2;  // lanes 32 * quarter .., columns half * BT / 2 ..
+        const int quarter = warp & 3, half = (warp - 2) >> 2;  // lanes 32 * quarter .., every other 32 columns
         uint32_t local = 0;
         for (int64_t tile = first; tile < tiles; tile += step, ++local) {
             int32_t n0, t0;
@@ -676,13 +684,13 @@ __global__ void __launch_bounds__(kPairThreads)
             lost = __any_sync(kFullMask, lost);
             if (lost) break;
             mma_fence_after();
-            const uint32_t row = tmem + ((uint32_t)(32 * quarter) << 16) + side * BT;
+            const uint32_t row = tmem + ((uint32_t)(32 * quarter) << 16) + side * 256;
 #pragma unroll 1
-            for (int c = half * (BT / 2); c < (half + 1) * (BT / 2); c += 32) {
+            for (int c = 32 * half; c < tokens; c += 64) {
                 if (t0 + c >= a.rows) break;
                 int32_t v[32];
                 tmem_load32(row + c, v);
-                store_columns<DT>(a, v, t0 + c, n, ws, bias);
+                store_columns<DT>(a, v, t0 + c, a.rows - t0 - c, n, ws, bias);
             }
             mma_fence_before();
             __syncwarp();
@@ -695,7 +703,7 @@ __global__ void __launch_bounds__(kPairThreads)
     __syncthreads();
     cluster_sync();  // nothing of the pair is in flight any more
     mma_fence_after();
-    if (warp == 1) tmem_free<true>(tmem, Cfg::kColumns);
+    if (warp == 1) tmem_free<true>(tmem, kPairColumns);
 }
 
 // ================= host side =================
@@ -724,28 +732,38 @@ bool make_map(CUtensorMap* map, const int8_t* p, int64_t rows, int64_t k, int64_
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int BT, int DT>
-bool launch_tile(const LinearArgs& a, int split, int dev, cudaStream_t st) {
-    static std::atomic<uint64_t> done{0};
-    typedef TileCfg<BT> Cfg;
-    if (!allow_shared(k_linear_tile<BT, DT>, Cfg::kShared, done, dev)) return false;
-    CUtensorMap wmap, xmap;
-    if (!make_map(&wmap, a.wq, a.n, a.k, a.ldw, kTileRows) || !make_map(&xmap, a.xq, a.rows, a.k, a.ldx, BT)) return false;
-    const int32_t t_tiles = (a.rows + BT - 1) / BT, n_tiles = (a.n + kTileRows - 1) / kTileRows;
-    return launch_chained(k_linear_tile<BT, DT>, (unsigned)((int64_t)t_tiles * n_tiles * split), kTileThreads2, Cfg::kShared, st, (unsigned)split, a, wmap, xmap, t_tiles,
-                          (int32_t)split);
+constexpr uint32_t kSharedLimit = 227 * 1024;
+
+TilePlan tile_plan(int32_t rows, int tokens, int split) {
+    TilePlan plan{tokens, (rows + tokens - 1) / tokens, split, kMaxStages};
+    const uint32_t room = tokens <= 64 ? kSharedLimit / 2 - 1024 : kSharedLimit;  // small tiles leave room for two CTAs an SM
+    while (plan.stages > 2 && plan.shared_bytes() > room) --plan.stages;
+    return plan;
 }
 
-template <int BT, int DT>
-bool launch_pair(const LinearArgs& a, int n_sm, int dev, cudaStream_t st) {
+template <int DT>
+bool launch_tile(const LinearArgs& a, int tokens, int split, int dev, cudaStream_t st) {
     static std::atomic<uint64_t> done{0};
-    typedef PairCfg<BT> Cfg;
-    if (!allow_shared(k_linear_pair<BT, DT>, Cfg::kShared, done, dev)) return false;
+    if (!allow_shared(k_linear_tile<DT>, kSharedLimit, done, dev)) return false;
     CUtensorMap wmap, xmap;
-    if (!make_map(&wmap, a.wq, a.n, a.k, a.ldw, kTileRows) || !make_map(&xmap, a.xq, a.rows, a.k, a.ldx, BT / 2)) return false;
-    const int64_t tiles = (int64_t)((a.rows + BT - 1) / BT) * ((a.n + 2 * kTileRows - 1) / (2 * kTileRows));
+    if (!make_map(&wmap, a.wq, a.n, a.k, a.ldw, kTileRows) || !make_map(&xmap, a.xq, a.rows, a.k, a.ldx, (uint32_t)tokens)) return false;
+    const TilePlan plan = tile_plan(a.rows, tokens, split);
+    const int32_t n_tiles = (a.n + kTileRows - 1) / kTileRows;
+    return launch_chained(k_linear_tile<DT>, (unsigned)((int64_t)plan.t_tiles * n_tiles * split), kTileThreads2, plan.shared_bytes(), st, (unsigned)split, a, wmap,
+                          xmap, plan);
+}
+
+template <int DT>
+bool launch_pair(const LinearArgs& a, int tokens, int n_sm, int dev, cudaStream_t st) {
+    static std::atomic<uint64_t> done{0};
+    if (!allow_shared(k_linear_pair<DT>, kSharedLimit, done, dev)) return false;
+    CUtensorMap wmap, xmap;
+    if (!make_map(&wmap, a.wq, a.n, a.k, a.ldw, kTileRows) || !make_map(&xmap, a.xq, a.rows, a.k, a.ldx, (uint32_t)tokens / 2)) return false;
+    const int64_t tiles = (int64_t)((a.rows + tokens - 1) / tokens) * ((a.n + 2 * kTileRows - 1) / (2 * kTileRows));
     const unsigned grid = 2 * (unsigned)std::min<int64_t>(tiles, n_sm / 2);
-    return launch_chained(k_linear_pair<BT, DT>, grid, kPairThreads, Cfg::kShared, st, 2, a, wmap, xmap);
+    const uint32_t stage = kWeightBytes + (uint32_t)tokens / 2 * kBlockK;
+    const int stages = std::min<int>(kMaxStages, (int)((kSharedLimit - kSharedHead - 1024) / stage));
+    return launch_chained(k_linear_pair<DT>, grid, kPairThreads, kSharedHead + stages * stage + 1024, st, 2, a, wmap, xmap, (int32_t)tokens, (int32_t)stages);
 }
 
 template <int M, int DT>
@@ -784,33 +802,57 @@ bool launch_few(const LinearArgs& a, int n_sm, cudaStream_t st) {
     return launch_chained(kernel, grid, 32 * kRowsWarps, 0, st, 1, a, parts);
 }
 
-// Which kernel: `tokens` of a tile (0: k_linear_rows), over one CTA or a pair, columns split so many ways.
+// Which kernel: `tokens` of a tile (0: k_linear_rows, 8: k_linear_few), over one CTA or a pair, columns split so many ways.
 struct Choice {
     int tokens, pair, split;
 };
 
+// The cheapest by a model of the kernels' time in clocks at 1.9 GHz, fitted to sweeps over 1 .. 8192 tokens and 300 .. 14336 columns
+// and channels.  What it says, with both sides measured (us):
+//   - a tile kernel's stage costs what its bytes take from L2, about 60 B a clock into one SM (k_linear_tile, up to 148 of them) or 44
+//     (k_linear_pair, all SMs at once); rows that do not start on 128 bytes cost half as much again: 333 x 4096 -> 2741 tokens and
+//     channels at a row distance of 5120 14.2, at 5008 18.8.  Hence large tiles for many tokens (2048 x 4096 x 4096: pair of 256
+//     tokens 26.8, of 128 39.1), and hence splits, which put every SM to work where there are few tiles (64 x 4096 x 4096: one
+//     CTA a tile 10.2, columns over four 7.4).
+//   - k_linear_few pays for each 8 tokens in warp-wide products: 16 x 4096 x 4096 5.9 against 7.6 in tiles, 24 x 4096 x 14336 19.8
+//     against 13.9.
 Choice choose(const LinearArgs& a, int n_sm) {
     if (a.k == 0 || a.rows <= 1) return {0, 0, 1};
-    if (a.rows <= 32) return {8, 0, 1};
-    const int64_t channels = (a.n + kTileRows - 1) / kTileRows, blocks = (a.k + kBlockK - 1) / kBlockK;
-    auto tiles = [&](int bt) { return channels * ((a.rows + bt - 1) / bt); };
-    if (a.rows > 128 && tiles(256) >= n_sm) return {256, 1, 1};
-    const int bt = a.rows <= 32 ? 32 : a.rows <= 64 ? 64 : 128;
-    int split = 1;
-    while (split < 8 && tiles(bt) * split * 2 <= n_sm + n_sm / 2 && blocks >= 4 * split) split *= 2;
-    return {bt, 0, split};
+    const double bytes = (double)a.n * a.k, memory = bytes / 3400.0;  // 6.5 TB/s
+    const double blocks = (a.k + kBlockK - 1) / kBlockK, rough = (a.ldw | a.ldx) % 128 ? 1.45 : 1.0;
+    Choice best{8, 0, 1};
+    double least = 1e300;
+    if (a.rows <= 32) least = 3300.0 + bytes * 1e-6 * 1900.0 * (0.15 + 0.052 * ((a.rows + 7) / 8));
+    const int64_t channels = (a.n + kTileRows - 1) / kTileRows, pairs = (a.n + 2 * kTileRows - 1) / (2 * kTileRows);
+    const int most = std::min(256, (a.rows + 31) / 32 * 32);
+    for (int tokens = 32; tokens <= most; tokens += 32) {
+        const int64_t t_tiles = (a.rows + tokens - 1) / tokens, tiles = channels * t_tiles;
+        const double stage = rough * std::max(std::max((16384.0 + 128.0 * tokens) / 60.0, 2.0 * tokens), 430.0);
+        static const int splits[] = {1, 2, 3, 4, 6, 8};
+        for (int split : splits) {
+            const int64_t turns = (tiles * split + n_sm - 1) / n_sm;
+            if (tokens % (4 * split)) continue;
+            if (split > 1 && (turns > 1 || blocks < 2 * split)) break;
+            const double late = 2600.0 / tile_plan(a.rows, tokens, split).stages;  // a stage's way from L2 to the product and back
+            const double cost = 5700.0 + std::max(memory, turns * (std::ceil(blocks / split) * std::max(stage, late))) + 30.0 * turns * tokens / split +
+                                (split > 1 ? 2500.0 + 10.0 * tokens + 350.0 * split : 0.0);
+            if (cost < least) least = cost, best = {tokens, 0, split};
+            if (tiles >= n_sm) break;
+        }
+        if (tokens < 64) continue;
+        const int64_t turns = (pairs * t_tiles + n_sm / 2 - 1) / (n_sm / 2);
+        const double pair_stage = std::max(rough * (16384.0 + 64.0 * tokens) / 44.0, 2.0 * tokens);
+        const double cost = 6500.0 + std::max(memory, turns * blocks * pair_stage) + 15.0 * tokens;
+        if (cost < least) least = cost, best = {tokens, 1, 1};
+    }
+    return best;
 }
 
 template <int DT>
 bool launch_linear(const LinearArgs& a, const Choice& c, int n_sm, int dev, cudaStream_t st) {
     if (c.tokens == 0) return launch_rows<DT>(a, n_sm, st);
     if (c.tokens == 8) return launch_few<DT>(a, n_sm, st);
-    if (c.pair) return c.tokens == 256 ? launch_pair<256, DT>(a, n_sm, dev, st) : launch_pair<128, DT>(a, n_sm, dev, st);
-    switch (c.tokens) {
-        case 32: return launch_tile<32, DT>(a, c.split, dev, st);
-        case 64: return launch_tile<64, DT>(a, c.split, dev, st);
-        default: return launch_tile<128, DT>(a, c.split, dev, st);
-    }
+    return c.pair ? launch_pair<DT>(a, c.tokens, n_sm, dev, st) : launch_tile<DT>(a, c.tokens, c.split, dev, st);
 }
 
 }  // namespace
