@@ -819,7 +819,7 @@ struct Choice {
 Choice choose(const LinearArgs& a, int n_sm) {
     if (a.k == 0 || a.rows <= 1) return {0, 0, 1};
     const double bytes = (double)a.n * a.k, memory = bytes / 3400.0;  // 6.5 TB/s
-    const double blocks = (a.k + kBlockK - 1) / kBlockK, rough = (a.ldw | a.ldx) % 128 ? 1.45 : 1.0;
+    const double blocks = (a.k + kBlockK - 1) / kBlockK, rough_w = a.ldw % 128 ? 1.45 : 1.0, rough_x = a.ldx % 128 ? 1.45 : 1.0;
     Choice best{8, 0, 1};
     double least = 1e300;
     if (a.rows <= 32) least = 3300.0 + bytes * 1e-6 * 1900.0 * (0.15 + 0.052 * ((a.rows + 7) / 8));
@@ -827,7 +827,7 @@ Choice choose(const LinearArgs& a, int n_sm) {
     const int most = std::min(256, (a.rows + 31) / 32 * 32);
     for (int tokens = 32; tokens <= most; tokens += 32) {
         const int64_t t_tiles = (a.rows + tokens - 1) / tokens, tiles = channels * t_tiles;
-        const double stage = rough * std::max(std::max((16384.0 + 128.0 * tokens) / 60.0, 2.0 * tokens), 430.0);
+        const double stage = std::max(std::max((rough_w * 16384.0 + rough_x * 128.0 * tokens) / 60.0, 2.0 * tokens), 430.0);
         static const int splits[] = {1, 2, 3, 4, 6, 8};
         for (int split : splits) {
             const int64_t turns = (tiles * split + n_sm - 1) / n_sm;
@@ -841,7 +841,7 @@ Choice choose(const LinearArgs& a, int n_sm) {
         }
         if (tokens < 64) continue;
         const int64_t turns = (pairs * t_tiles + n_sm / 2 - 1) / (n_sm / 2);
-        const double pair_stage = std::max(rough * (16384.0 + 64.0 * tokens) / 44.0, 2.0 * tokens);
+        const double pair_stage = std::max((rough_w * 16384.0 + rough_x * 64.0 * tokens) / 44.0, 2.0 * tokens);
         const double cost = 6500.0 + std::max(memory, turns * blocks * pair_stage) + 15.0 * tokens;
         if (cost < least) least = cost, best = {tokens, 1, 1};
     }

@@ -805,7 +805,7 @@ int64_t launch_norm_backward(const NormBackArgs& a, cudaStream_t st) {
     const size_t row_bytes = ((size_t)a.cols * (DT == DNNS_F32 ? 4 : 2) + 15) / 16 * 16 + (VEC ? 0 : 16), stage = 3 * row_bytes * s.teams;
     int blocks = norm_backward_blocks(s);
     while (blocks > 1 && kRoom / blocks < 3 * stage) --blocks;
-    const int stages = (int)std::min<size_t>(4, kRoom / blocks / stage);
+    const int stages = (int)std::min<size_t>(3, kRoom / blocks / stage);
     if (s.nv == 0 || stages < 2) {
         const int64_t grid = std::min<int64_t>(a.rows, 148);
         return launch_chained(k_norm_backward_long<DT, VEC>, (unsigned)grid, 512, 0, st, 1, a) ? grid : -1;

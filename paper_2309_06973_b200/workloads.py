@@ -426,3 +426,24 @@ def freeze_streams(wl: Workload) -> Workload:
 
 
 BY_NAME = {"toy": toy, "vgg16": vgg16, "resnet56": resnet56, "resnet50": resnet50, "resnet152": resnet152}
+
+
+def gated_block(width: int, hidden: int, seed: int = 0, prune=(1, 2)) -> Workload:
+    """The feed-forward block of a language model, y = down(silu(gate(x)) * up(x)): three matrices around one group of hidden
+    units, whose sizes vary (a log-normal factor a unit, shared by its two producers and its consumer), so that a share of them
+    vanishes whole when the prune[0] / prune[1] least weights are masked."""
+    b = _Builder()
+    g_in, g_hidden, g_out = b.group(width, frozen=True), b.group(hidden), b.group(width, frozen=True)
+    for name, gi, go in (("gate", g_in, g_hidden), ("up", g_in, g_hidden), ("down", g_hidden, g_out)):
+        b.tensors.append(TensorSpec(name, b.groups[go].C, b.groups[gi].C, 1, 1, go, gi))
+    wl = Workload(f"gated_block_{width}x{hidden}", seed, SCOPE_GLOBAL, b.tensors, [], b.groups, [], 1)
+    rng = np.random.default_rng(seed)
+    unit = np.exp(2.0 * rng.standard_normal(hidden)).astype(np.float32)
+    for t in wl.tensors:
+        w = rng.standard_normal((t.O, t.I, 1, 1), dtype=np.float32) * np.float32(t.I ** -0.5)
+        w *= unit[:, None, None, None] if t.out_group == g_hidden else unit[None, :, None, None]
+        wl.weights.append(np.ascontiguousarray(w))
+        wl.biases.append(None)
+    wl.planted = [np.zeros(0, np.int64) for _ in wl.tensors]
+    wl.ks = np.array([[k_fraction(wl.n_prunable, *prune)]], np.uint64)
+    return wl
