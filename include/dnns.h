@@ -456,7 +456,7 @@ dnns_status dnns_inflate(const void* stream_dev, size_t stream_bytes, const uint
  *   - Outputs do not overlap inputs, except where a call says so.  rows == 0 does nothing (a gradient that is a sum over
  *     rows is then zero); cols == 0 gives scale 0 for every row.
  *   - Errors: INVALID_ARG (null or misaligned pointer, negative size, an ld below its columns, eps), UNSUPPORTED
- *     (dtype; more than 2^31 - 1 rows, or columns: 2^30 in a matrix of values; a matrix of 2^62 bytes or more), CUDA.
+ *     (dtype; more than 2^31 - 1 rows or 2^30 columns; a matrix of 2^62 bytes or more), CUDA.
  */
 size_t dnns_quantized_row_bytes(size_t cols); /* cols rounded up to a multiple of 16 */
 
@@ -501,7 +501,8 @@ dnns_status dnns_silu_gate_backward(const void* dy, int64_t lddy, const void* ga
 
 /*
  * Product of rows in 8 bits:  y[t][n] = (sum_k xq[t][k] * wq[n][k]) * xscale[t] * wscale[n] + bias[n]
- * for rows tokens, in_cols columns and out_cols output channels; y has element type dtype, rows of ldy elements; bias
+ * for rows tokens, in_cols columns and out_cols output channels (UNSUPPORTED: more than 2^30 tokens or channels); y has
+ * element type dtype, rows of ldy elements; bias
  * (fp32, nullable).  The sum is exact: in_cols is at most DNNS_LINEAR_MAX_IN (UNSUPPORTED above), so that int32 holds it.
  * in_cols == 0 leaves the bias.  Every wait of the kernels is bounded; one that runs out ends the kernel, leaves y
  * incomplete and sets *status_dev (device word, cleared by the caller) to DNNS_ERR_TIMEOUT.

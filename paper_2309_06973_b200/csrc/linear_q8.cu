@@ -54,11 +54,13 @@ __device__ __forceinline__ float scaled(int32_t acc, float xs, float ws, float b
 // The tokens are read beside them, from the L1 cache but for a block's first warp (the weights pass it by).
 constexpr int kRowsWarps = 8;
 
+// (Not the read-only path, here and for the tokens: a chained kernel begins while the one that writes them may still run.)
 __device__ __forceinline__ int4 stream16(const int8_t* p) {
     int4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
 }
+__device__ __forceinline__ int4 token16(const int8_t* p) { return *reinterpret_cast<const int4*>(p); }
 __device__ __forceinline__ int32_t dot16(const int4& a, const int4& b, int32_t c) { return __dp4a(a.x, b.x, __dp4a(a.y, b.y, __dp4a(a.z, b.z, __dp4a(a.w, b.w, c)))); }
 
 // M tokens at most (a.rows of them), blockIdx.y the token group.
@@ -93,7 +95,7 @@ __global__ void __launch_bounds__(32 * kRowsWarps) k_linear_rows(const LinearArg
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int t = 0; t < M; ++t) {
-                const int4 xv = __ldg(reinterpret_cast<const int4*>(x[t] + 16 * (v + u * step)));
+                const int4 xv = token16(x[t] + 16 * (v + u * step));
 #pragma unroll
                 for (int i = 0; i < R; ++i) acc[i][t] = dot16(wv[u][i], xv, acc[i][t]);
             }
@@ -104,7 +106,7 @@ __global__ void __launch_bounds__(32 * kRowsWarps) k_linear_rows(const LinearArg
         for (int i = 0; i < R; ++i) wv[i] = stream16(w[i] + 16 * v);
 #pragma unroll
         for (int t = 0; t < M; ++t) {
-            const int4 xv = __ldg(reinterpret_cast<const int4*>(x[t] + 16 * v));
+            const int4 xv = token16(x[t] + 16 * v);
 #pragma unroll
             for (int i = 0; i < R; ++i) acc[i][t] = dot16(wv[i], xv, acc[i][t]);
         }
@@ -195,12 +197,12 @@ __global__ void __launch_bounds__(32 * kRowsWarps, 2) k_linear_few(const LinearA
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int t = 0; t < TB; ++t) lane_product(acc[t], wl[u], wh[u], __ldg(reinterpret_cast<const int4*>(x[t] + 64 * (b + u * step) + 16 * q)));
+            for (int t = 0; t < TB; ++t) lane_product(acc[t], wl[u], wh[u], token16(x[t] + 64 * (b + u * step) + 16 * q));
     }
     for (; b < whole; b += step) {
         const int4 wl = stream16(lo + 64 * b + 16 * q), wh = stream16(hi + 64 * b + 16 * q);
 #pragma unroll
-        for (int t = 0; t < TB; ++t) lane_product(acc[t], wl, wh, __ldg(reinterpret_cast<const int4*>(x[t] + 64 * b + 16 * q)));
+        for (int t = 0; t < TB; ++t) lane_product(acc[t], wl, wh, token16(x[t] + 64 * b + 16 * q));
     }
     if (part == parts - 1 && (a.k & 63)) {
         const int32_t c = 64 * whole + 16 * q;
@@ -866,7 +868,7 @@ extern "C" dnns_status dnns_linear_quantized(const int8_t* xq, int64_t ldx, cons
     auto address = [](const void* p) { return reinterpret_cast<uintptr_t>(p); };
     if (rows < 0 || in_cols < 0 || out_cols < 0) return DNNS_ERR_INVALID_ARG;
     if (dtype != DNNS_F32 && dtype != DNNS_BF16) return DNNS_ERR_UNSUPPORTED;
-    const int64_t limit = (int64_t)1 << 31, span = (int64_t)1 << 60;
+    const int64_t limit = ((int64_t)1 << 30) + 1, span = (int64_t)1 << 60;
     if (rows >= limit || out_cols >= limit || in_cols > DNNS_LINEAR_MAX_IN) return DNNS_ERR_UNSUPPORTED;
     if (!status_dev || address(status_dev) % 4) return DNNS_ERR_INVALID_ARG;
     if (rows == 0 || out_cols == 0) return DNNS_OK;

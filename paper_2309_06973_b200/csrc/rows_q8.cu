@@ -669,7 +669,7 @@ __global__ void __launch_bounds__(512) k_norm_backward_long(const NormBackArgs a
 }
 
 // dweight[c] = sum of the teams' partial sums in a fixed order: 8 columns (a sector) by 32 runs of teams a block.
-__global__ void __launch_bounds__(256) k_norm_weight_sum(const float* __restrict__ part, int64_t teams, int64_t cols, float* __restrict__ dweight) {
+__global__ void __launch_bounds__(256) k_norm_weight_sum(const float* part, int64_t teams, int64_t cols, float* dweight) {
     chain_go();
     chain_wait();
     __shared__ float s[32][9];

@@ -29,6 +29,7 @@ struct Rows {
     float* scale;
     uint16_t* values;
     int64_t ldq, ldv, rows, cols;
+    int64_t device;
 };
 PyTypeObject RowsType = {PyVarObject_HEAD_INIT(nullptr, 0)};
 
@@ -90,9 +91,14 @@ bool vector_or_none(PyObject* o, int64_t n, const char* what, float** p) {
 }
 
 Rows* rows_of(PyObject* o) {
-    if (Py_TYPE(o) == &RowsType) return reinterpret_cast<Rows*>(o);
-    refuse("rows", "rows in 8 bits", o);
-    return nullptr;
+    if (Py_TYPE(o) != &RowsType) return refuse("rows", "rows in 8 bits", o), nullptr;
+    return reinterpret_cast<Rows*>(o);
+}
+// (after a tensor of the call was found on the current device)
+bool rows_here(const Rows* r) {
+    if (r->device == c10::cuda::current_device()) return true;
+    PyErr_SetString(PyExc_ValueError, "rows: rows of the current CUDA device are needed");
+    return false;
 }
 
 void* stream() { return c10::cuda::getCurrentCUDAStream().stream(); }
@@ -115,18 +121,18 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Py_RETURN_NONE;
 }
 
-// rows(q, ldq, scale, values, ldv, rows, cols): all integers
+// rows(q, ldq, scale, values, ldv, rows, cols, device): all integers
 PyObject* rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (!count_is(n, 7)) return nullptr;
-    long long v[7];
-    for (int i = 0; i < 7; ++i) {
+    if (!count_is(n, 8)) return nullptr;
+    long long v[8];
+    for (int i = 0; i < 8; ++i) {
         v[i] = PyLong_AsLongLong(a[i]);
         if (v[i] == -1 && PyErr_Occurred()) return nullptr;
     }
     Rows* r = PyObject_New(Rows, &RowsType);
     if (!r) return nullptr;
     r->q = reinterpret_cast<int8_t*>(v[0]), r->ldq = v[1], r->scale = reinterpret_cast<float*>(v[2]), r->values = reinterpret_cast<uint16_t*>(v[3]);
-    r->ldv = v[4], r->rows = v[5], r->cols = v[6];
+    r->ldv = v[4], r->rows = v[5], r->cols = v[6], r->device = v[7];
     return reinterpret_cast<PyObject*>(r);
 }
 
@@ -136,7 +142,8 @@ PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
     at::ScalarType type;
     int32_t dtype;
     Matrix x;
-    if (!count_is(n, 2) || !(r = rows_of(a[1])) || !dtype_of(a[0], "x", &type, &dtype) || !matrix(a[0], r->rows, r->cols, type, "x", &x)) return nullptr;
+    if (!count_is(n, 2) || !(r = rows_of(a[1])) || !dtype_of(a[0], "x", &type, &dtype) || !matrix(a[0], r->rows, r->cols, type, "x", &x) || !rows_here(r))
+        return nullptr;
     return status(g_calls.quantize_rows(x.p, x.ld, dtype, r->rows, r->cols, r->q, r->ldq, r->scale, r->values, r->ldv, stream()));
 }
 
@@ -149,7 +156,7 @@ PyObject* rmsnorm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     float* w;
     if (!count_is(n, 6) || !(r = rows_of(a[3])) || !dtype_of(a[0], "x", &type, &dtype) || !matrix(a[0], r->rows, r->cols, type, "x", &x) ||
         !vector_or_none(a[1], r->cols, "weight", &w) || !matrix_or_none(a[4], r->rows, r->cols, type, "residual", &res) ||
-        !matrix_or_none(a[5], r->rows, r->cols, type, "h", &h))
+        !matrix_or_none(a[5], r->rows, r->cols, type, "h", &h) || !rows_here(r))
         return nullptr;
     const double eps = PyFloat_AsDouble(a[2]);
     if (eps == -1.0 && PyErr_Occurred()) return nullptr;
@@ -188,7 +195,7 @@ PyObject* silu_gate(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int32_t dtype;
     Matrix g, u;
     if (!count_is(n, 3) || !(r = rows_of(a[2])) || !dtype_of(a[0], "gate", &type, &dtype) || !matrix(a[0], r->rows, r->cols, type, "gate", &g) ||
-        !matrix(a[1], r->rows, r->cols, type, "up", &u))
+        !matrix(a[1], r->rows, r->cols, type, "up", &u) || !rows_here(r))
         return nullptr;
     return status(g_calls.silu_gate_quantize(g.p, g.ld, u.p, u.ld, dtype, r->rows, r->cols, r->q, r->ldq, r->scale, r->values, r->ldv, stream()));
 }
@@ -214,7 +221,7 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Matrix y;
     float* bias;
     if (!count_is(n, 5) || !(x = rows_of(a[0])) || !(w = rows_of(a[1])) || !vector_or_none(a[2], w->rows, "bias", &bias) ||
-        !dtype_of(a[3], "y", &type, &dtype) || !matrix(a[3], x->rows, w->rows, type, "y", &y))
+        !dtype_of(a[3], "y", &type, &dtype) || !matrix(a[3], x->rows, w->rows, type, "y", &y) || !rows_here(x) || !rows_here(w))
         return nullptr;
     if (x->cols != w->cols) return PyErr_Format(PyExc_ValueError, "x has %lld columns, the layer %lld", (long long)x->cols, (long long)w->cols);
     uint32_t* where = static_cast<uint32_t*>(PyLong_AsVoidPtr(a[4]));
@@ -222,7 +229,19 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return status(g_calls.linear_quantized(x->q, x->ldq, x->scale, w->q, w->ldq, w->scale, bias, x->rows, x->cols, w->rows, dtype, y.p, y.ld, where, stream()));
 }
 
-#define DNNS_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
+// torch reports by exceptions (no device, a tensor without storage): they end here
+template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
+PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    try {
+        return F(self, a, n);
+    } catch (const std::exception& e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+    } catch (...) {
+        PyErr_SetString(PyExc_RuntimeError, "unknown error");
+    }
+    return nullptr;
+}
+#define DNNS_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<name>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {DNNS_METHOD(bind),      DNNS_METHOD(rows),      DNNS_METHOD(quantize_rows),      DNNS_METHOD(rmsnorm), DNNS_METHOD(rmsnorm_backward),
                          DNNS_METHOD(silu_gate), DNNS_METHOD(silu_gate_backward), DNNS_METHOD(linear), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "Calls on rows in 8 bits from torch tensors.", -1, methods};

@@ -437,7 +437,7 @@ class RowsQ8:
         self.rows, self.cols, self.q, self.scale, self.values, self.device = rows, cols, q, scale, values, q.device
         self._c = _native.rows(q.data_ptr(), q.stride(0) if rows > 1 else B.dnns_quantized_row_bytes(cols), scale.data_ptr(),
                                0 if values is None else values.data_ptr(),
-                               0 if values is None else values.stride(0) if rows > 1 else cols, rows, cols)
+                               0 if values is None else values.stride(0) if rows > 1 else cols, rows, cols, q.get_device())
 
 
 def quantize_rows(x: torch.Tensor, out: RowsQ8) -> RowsQ8:

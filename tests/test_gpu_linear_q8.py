@@ -154,6 +154,74 @@ def test_repeated_calls_streams_and_graphs(rows):
     assert torch.equal(y, first) and layer.device_status() == B.DNNS_OK
 
 
+@pytest.mark.parametrize("tokens", [1, 8, 40, 300])
+def test_chains_of_calls_see_each_others_results(tokens):
+    """Norm -> product -> gated activation -> product over the same buffers, call after call without waiting, from a stream
+    and from a graph: each link begins before the one in front of it has ended, and must still read what that one wrote."""
+    width, hidden, rounds = 1040, 700, 40
+    g = gen(tokens)
+    gate_up, down = R.LinearQ8(rows8(2 * hidden, width, 1)), R.LinearQ8(rows8(width, hidden, 2))
+    n, a = R.RowsQ8(tokens, width), R.RowsQ8(tokens, hidden)
+    gu, h = torch.empty(tokens, 2 * hidden, dtype=BF16, device="cuda"), torch.empty(tokens, width, dtype=BF16, device="cuda")
+    xs = torch.randn(rounds, tokens, width, generator=g, device="cuda").to(BF16)
+
+    def step(x, y, wait=lambda: None):
+        for call in (lambda: R.rmsnorm_q8(x, None, 1e-6, n, residual=x, h=h), lambda: gate_up(n, gu),
+                     lambda: R.silu_gate_q8(gu[:, :hidden], gu[:, hidden:], a), lambda: down(a, y)):
+            call()
+            wait()
+
+    want, got = torch.empty_like(xs), torch.zeros_like(xs)
+    for x, y in zip(xs, want):
+        step(x, y, torch.cuda.synchronize)
+    for _ in range(3):
+        for x, y in zip(xs, got):
+            step(x, y)
+        assert torch.equal(got, want)
+        got.zero_()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            for x, y in zip(xs, got):
+                step(x, y)
+        for _ in range(3):
+            got.zero_()
+            graph.replay()
+        side.synchronize()
+    assert torch.equal(got, want) and gate_up.device_status() == B.DNNS_OK == down.device_status()
+
+
+def test_fork_and_join_in_a_capture():
+    """Two branches of a captured graph with the calls in both, then one that needs both."""
+    x, w = rows8(64, 1000, 1), rows8(500, 1000, 2)
+    ys = [torch.empty(64, 500, dtype=BF16, device="cuda") for _ in range(2)]
+    layers, out = [R.LinearQ8(w) for _ in range(2)], R.RowsQ8(64, 500, values=True)
+    main, side = torch.cuda.Stream(), torch.cuda.Stream()
+
+    def both():
+        layers[0](x, ys[0])
+        side.wait_stream(main)
+        layers[0](x, ys[0])
+        with torch.cuda.stream(side):
+            layers[1](x, ys[1])
+        main.wait_stream(side)
+        R.silu_gate_q8(ys[0], ys[1], out)
+
+    with torch.cuda.stream(main):
+        both()
+        main.synchronize()
+        want = out.q.clone()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=main):
+            both()
+        for _ in range(20):
+            ys[0].zero_(), ys[1].zero_(), out.q.zero_()
+            graph.replay()
+            main.synchronize()
+            assert torch.equal(out.q[:, :500], want[:, :500])
+
+
 def test_offsets_past_32_bits():
     """Output rows so far apart that the last ones start past 2^32 elements."""
     ld, rows, n = (1 << 30) + 3, 5, 40

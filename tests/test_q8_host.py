@@ -93,11 +93,11 @@ def test_native_calls_refuse_what_is_not_on_the_device():
     import torch
 
     from paper_2309_06973_b200 import runtime as R
-    rows = R._native.rows(A, 16, A, 0, 0, 2, 3)
+    rows = R._native.rows(A, 16, A, 0, 0, 2, 3, 0)
     x = torch.zeros(2, 3)
     for call in (lambda: R._native.quantize_rows(x, rows), lambda: R._native.rmsnorm(x, None, 1e-5, rows, None, None),
                  lambda: R._native.silu_gate(x, x, rows), lambda: R._native.rmsnorm_backward(x, x, None, 1e-5, x, None, None, None),
-                 lambda: R._native.silu_gate_backward(x, x, x, x, x), lambda: R._native.linear(rows, R._native.rows(A, 16, A, 0, 0, 3, 3), None, x, A),
+                 lambda: R._native.silu_gate_backward(x, x, x, x, x), lambda: R._native.linear(rows, R._native.rows(A, 16, A, 0, 0, 3, 3, 0), None, x, A),
                  lambda: R._native.quantize_rows(x.t(), rows), lambda: R._native.quantize_rows(x.half(), rows),
                  lambda: R._native.quantize_rows("x", rows), lambda: R._native.quantize_rows(x, x), lambda: R.RowsQ8.of(x.to(torch.int8), x[:, 0], 3)):
         with pytest.raises(ValueError):
