@@ -356,17 +356,27 @@ __device__ __forceinline__ void tmem_load32(uint32_t at, int32_t (&v)[32]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
-// Up to 32 columns (tokens t0 .. t0 + left - 1) of one channel a lane: scale and store.
-template <int DT>
-__device__ __forceinline__ void store_columns(const LinearArgs& a, const int32_t (&v)[32], int32_t t0, int32_t left, int32_t n, float ws, float bias) {
+// Up to 32 columns (tokens t0 .. t0 + left - 1) of one channel a lane: scale and store.  The tokens' scales: a lane fetches one and
+// they go round by shuffles, or (SHARED) they are in shared memory.  Measured: in shared memory, fetched beside the
+// products, 200 x 4096 x 4096 over clusters of two 11.4 -> 10.2 us; but a whole tile's 128 to 256 columns stored without the shuffles'
+// pace between them take longer (4000 x 300 x 300 5.8 -> 7.6), so tiles of one CTA or a pair keep the shuffles.
+template <int DT, bool SHARED = false>
+__device__ __forceinline__ void store_columns(const LinearArgs& a, const int32_t (&v)[32], int32_t t0, int32_t left, int32_t n, float ws, float bias,
+                                              const float4* scales = nullptr) {
     typedef typename std::conditional<DT == DNNS_F32, float, uint16_t>::type T;
     const int lane = threadIdx.x & 31;
-    const float mine = lane < left ? a.xscale[t0 + lane] : 0.0f;
+    const float mine = !SHARED && lane < left ? a.xscale[t0 + lane] : 0.0f;
     T* y = static_cast<T*>(a.y) + (int64_t)t0 * a.ldy + n;
     const bool in = n < a.n;
 #pragma unroll
     for (int j = 0; j < 32; ++j) {
-        const float xs = __shfl_sync(kFullMask, mine, j);
+        float xs;
+        if constexpr (SHARED) {
+            const float4 four = scales[j / 4];
+            xs = j & 2 ? (j & 1 ? four.w : four.z) : (j & 1 ? four.y : four.x);
+        } else {
+            xs = __shfl_sync(kFullMask, mine, j);
+        }
         if (in && j < left) store_out<DT>(y, 0, scaled(v[j], xs, ws, bias));
         y += a.ldy;
     }
@@ -376,8 +386,9 @@ constexpr int kMaxStages = 10;
 struct TileShared {  // in front of the stages
     uint64_t full[kMaxStages], empty[kMaxStages], done[2], taken[2], drain;
     uint32_t tmem, gave_up;
+    alignas(16) float scales[128];  // of the tokens that a CTA of a cluster stores
 };
-constexpr uint32_t kSharedHead = 1024;
+constexpr uint32_t kSharedHead = 2048;
 static_assert(sizeof(TileShared) <= kSharedHead, "head of the shared memory");
 
 __device__ __forceinline__ unsigned char* shared_base() {
@@ -483,6 +494,9 @@ __global__ void __launch_bounds__(kTileThreads2) k_linear_tile(const LinearArgs 
     const int quarter = warp & 3;  // tensor memory lanes a warp may read: 32 * (its index mod 4) ..
     const int32_t n = n0 + 32 * quarter + lane;
     const float ws = warp >= 2 && n < a.n ? a.wscale[n] : 0.0f, bias = warp >= 2 && a.bias && n < a.n ? a.bias[n] : 0.0f;
+    const int share = plan.tokens / split, t1 = t0 + slice * share;  // the tokens that this CTA stores
+    if (split > 1)
+        for (int i = threadIdx.x; i < share; i += kTileThreads2) s.scales[i] = t1 + i < a.rows ? a.xscale[t1 + i] : 0.0f;
     // everybody waits for the sums: after this no copy and no product of this CTA is in flight
     __syncwarp();
     const bool ok = __shfl_sync(kFullMask, (int)(lane == 0 && mbar_wait(&s.done[0], 0, gave_up)), 0);
@@ -502,7 +516,6 @@ __global__ void __launch_bounds__(kTileThreads2) k_linear_tile(const LinearArgs 
     } else {
         // the cluster's CTAs share the columns out: CTA r gets everybody's sums of columns r * share .., four columns of a channel
         // in 16 bytes
-        const int share = plan.tokens / split;
         const uint32_t sums = smem_addr(base) + plan.sums_at();
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // (the barrier arrived at above)
         if (warp >= 2) {
@@ -528,7 +541,7 @@ __global__ void __launch_bounds__(kTileThreads2) k_linear_tile(const LinearArgs 
         cluster_sync();
         if (warp >= 2 && ok) {
             const int4* part = reinterpret_cast<const int4*>(base + plan.sums_at()) + 32 * quarter + lane;
-            const int32_t t1 = t0 + slice * share, have = min(share, a.rows - t1);
+            const int32_t have = min(share, a.rows - t1);
 #pragma unroll 1
             for (int c = 0; c < have; c += 32) {
                 int32_t v[32];
@@ -544,7 +557,7 @@ __global__ void __launch_bounds__(kTileThreads2) k_linear_tile(const LinearArgs 
                         v[j] += p.x, v[j + 1] += p.y, v[j + 2] += p.z, v[j + 3] += p.w;
                     }
                 }
-                store_columns<DT>(a, v, t1 + c, have - c, n, ws, bias);
+                store_columns<DT, true>(a, v, t1 + c, have - c, n, ws, bias, reinterpret_cast<const float4*>(s.scales + c));
             }
         }
     }
