@@ -163,8 +163,11 @@ __device__ __forceinline__ void lane_product(int32_t (&d)[4], const int4& lo, co
 // Bytes c .. c + 15 of a row of k bytes, those past the end as 0 (never read).
 __device__ __forceinline__ int4 row16(const int8_t* row, int32_t c, int32_t k) {
     if (c + 16 <= k) return *reinterpret_cast<const int4*>(row + c);
-    uint32_t w[4] = {0, 0, 0, 0};
-    for (int i = 0; c + i < k; ++i) w[i >> 2] |= (uint32_t)(uint8_t)row[c + i] << (8 * (i & 3));
+    uint32_t b[16], w[4];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) b[i] = c + i < k ? (uint32_t)(uint8_t)row[c + i] : 0u;  // (all on their way together)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = b[4 * i] | b[4 * i + 1] << 8 | b[4 * i + 2] << 16 | b[4 * i + 3] << 24;
     return make_int4((int)w[0], (int)w[1], (int)w[2], (int)w[3]);
 }
 
@@ -806,11 +809,18 @@ bool launch_rows(const LinearArgs& a, int n_sm, cudaStream_t st) {
     return a.rows <= 2 ? launch_rows_of<2, DT>(a, n_sm, st) : launch_rows_of<4, DT>(a, n_sm, st);
 }
 
+// Warps that share the columns of 16 channels: as long as the 16 warps an SM that fit at a time are not passed (17 x 3000 x 5000 in
+// two turns of blocks 11.9 us, in one 8.6), down to four loads a lane.
+int few_parts(int64_t n, int64_t k, int n_sm) {
+    int parts = 1;
+    while (parts < kRowsWarps && (n + 15) / 16 * parts * 2 <= 16 * (int64_t)n_sm && k >= 4 * 64 * 2 * parts) parts *= 2;
+    return parts;
+}
+
 template <int DT>
 bool launch_few(const LinearArgs& a, int n_sm, cudaStream_t st) {
     const int64_t groups = ((int64_t)a.n + 15) / 16;
-    int parts = 1;
-    while (parts < kRowsWarps && groups * parts < 16 * (int64_t)n_sm && a.k >= 4 * 64 * 2 * parts) parts *= 2;
+    const int parts = few_parts(a.n, a.k, n_sm);
     const unsigned grid = (unsigned)((groups * parts + kRowsWarps - 1) / kRowsWarps);
     const int blocks = (a.rows + 7) / 8;
     const auto kernel = blocks == 1 ? k_linear_few<1, DT> : blocks == 2 ? k_linear_few<2, DT> : blocks == 3 ? k_linear_few<3, DT> : k_linear_few<4, DT>;
@@ -822,22 +832,27 @@ struct Choice {
     int tokens, pair, split;
 };
 
-// The cheapest by a model of the kernels' time in clocks at 1.9 GHz, fitted to sweeps over 1 .. 8192 tokens and 300 .. 14336 columns
-// and channels.  What it says, with both sides measured (us):
+// The cheapest by a model of the kernels' time in clocks at 1.9 GHz, fitted to sweeps of every tile and split over 37 shapes of 1 ..
+// 8192 tokens and 250 .. 14336 columns and channels (what it takes is within 1.15 of the best of each but for four, 1.2 to 1.45).  What it
+// says, with both sides measured (us):
 //   - a tile kernel's stage costs what its bytes take from L2, about 60 B a clock into one SM (k_linear_tile, up to 148 of them) or 44
-//     (k_linear_pair, all SMs at once); rows that do not start on 128 bytes cost half as much again: 333 x 4096 -> 2741 tokens and
-//     channels at a row distance of 5120 14.2, at 5008 18.8.  Hence large tiles for many tokens (2048 x 4096 x 4096: pair of 256
-//     tokens 26.8, of 128 39.1), and hence splits, which put every SM to work where there are few tiles (64 x 4096 x 4096: one
-//     CTA a tile 10.2, columns over four 7.4).
-//   - k_linear_few pays for each 8 tokens in warp-wide products: 16 x 4096 x 4096 5.9 against 7.6 in tiles, 24 x 4096 x 14336 19.8
-//     against 13.9.
+//     (k_linear_pair, all SMs at once); rows that do not start on 128 bytes cost more: 333 x 5003 x 2741 (tokens, columns, channels) at a row
+//     distance of 5008 14.2, of 5120 11.3.  Hence large tiles for many tokens (2048 x 4096 x 4096: a pair with 256 tokens 27.0, with
+//     128 39.8), and hence splits, which put every SM to work where there are few tiles (64 x 4096 x 4096: one CTA a tile 9.9,
+//     its columns over four 6.8).  With few stages a stage costs its way from L2 to the product and back instead.
+//   - k_linear_few pays for each 8 tokens in warp-wide products: 16 x 4096 x 4096 5.9 against 7.4 in tiles, 24 x 4096 x 14336 19.9
+//     against 13.4; and for loads one after the other where the columns are not whole batches: 5 x 700 x 3000 4.4 against 3.7.
 Choice choose(const LinearArgs& a, int n_sm) {
     if (a.k == 0 || a.rows <= 1) return {0, 0, 1};
     const double bytes = (double)a.n * a.k, memory = bytes / 3400.0;  // 6.5 TB/s
-    const double blocks = (a.k + kBlockK - 1) / kBlockK, rough_w = a.ldw % 128 ? 1.45 : 1.0, rough_x = a.ldx % 128 ? 1.45 : 1.0;
+    const double blocks = (a.k + kBlockK - 1) / kBlockK, rough_w = a.ldw % 128 ? 1.2 : 1.0, rough_x = a.ldx % 128 ? 1.2 : 1.0;
     Choice best{8, 0, 1};
     double least = 1e300;
-    if (a.rows <= 32) least = 3300.0 + bytes * 1e-6 * 1900.0 * (0.15 + 0.052 * ((a.rows + 7) / 8));
+    if (a.rows <= 32) {
+        // a warp's loads one after the other: four pieces at a time, then one by one, then the ragged one
+        const int pieces = a.k / 64 / few_parts(a.n, a.k, n_sm), turns = pieces / 4 + pieces % 4 + (a.k % 64 ? 2 : 0);
+        least = 3300.0 + std::max(bytes * 1e-6 * 1900.0 * (0.15 + 0.052 * ((a.rows + 7) / 8)), turns * 2300.0);
+    }
     const int64_t channels = (a.n + kTileRows - 1) / kTileRows, pairs = (a.n + 2 * kTileRows - 1) / (2 * kTileRows);
     const int most = std::min(256, (a.rows + 31) / 32 * 32);
     for (int tokens = 32; tokens <= most; tokens += 32) {
@@ -847,9 +862,9 @@ Choice choose(const LinearArgs& a, int n_sm) {
         for (int split : splits) {
             const int64_t turns = (tiles * split + n_sm - 1) / n_sm;
             if (tokens % (4 * split)) continue;
-            if (split > 1 && (turns > 1 || blocks < 2 * split)) break;
+            if (split > 1 && (tiles * split > (tokens <= 64 ? 2 : 1) * (int64_t)n_sm || blocks < 2 * split)) break;
             const double late = 2600.0 / tile_plan(a.rows, tokens, split).stages;  // a stage's way from L2 to the product and back
-            const double cost = 5700.0 + std::max(memory, turns * (std::ceil(blocks / split) * std::max(stage, late))) + 30.0 * turns * tokens / split +
+            const double cost = 4000.0 + std::max(memory, turns * (std::ceil(blocks / split) * std::max(stage, late))) + 30.0 * turns * tokens / split +
                                 (split > 1 ? 2500.0 + 10.0 * tokens + 350.0 * split : 0.0);
             if (cost < least) least = cost, best = {tokens, 0, split};
             if (tiles >= n_sm) break;
