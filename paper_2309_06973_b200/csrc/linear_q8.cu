@@ -64,6 +64,8 @@ __device__ __forceinline__ int4 token16(const int8_t* p) { return *reinterpret_c
 __device__ __forceinline__ int32_t dot16(const int4& a, const int4& b, int32_t c) { return __dp4a(a.x, b.x, __dp4a(a.y, b.y, __dp4a(a.z, b.z, __dp4a(a.w, b.w, c)))); }
 
 // M tokens at most (a.rows of them), blockIdx.y the token group.
+// 1 x 4096 x 4096 (tokens, columns, channels): 3.0 us with the weights in L2, 4.6 with them in HBM (floor 2.6, and 1.7 of that time is
+// what any kernel of this size takes); 1 x 4096 x 14336 11.2 (5.2 TB/s, floor 9.0); 1 x 1024 x 1024 1.8.
 template <int M, int R, int DT>
 __global__ void __launch_bounds__(32 * kRowsWarps) k_linear_rows(const LinearArgs a, int32_t parts) {
     chain_go();
@@ -171,7 +173,9 @@ __device__ __forceinline__ int4 row16(const int8_t* row, int32_t c, int32_t k) {
     return make_int4((int)w[0], (int)w[1], (int)w[2], (int)w[3]);
 }
 
-// 8 * TB tokens at most (a.rows of them)
+// 8 * TB tokens at most (a.rows of them): a warp has 16 channels, on the rows of its products, and all the tokens on the columns.
+// Bound by the weights' way like the kernel above, and for more tokens by the products' issue and the tokens read from L1 for each
+// 16 channels: 16 x 4096 x 4096 5.9 us (floor 2.6), 5 x 700 x 3000 4.4.
 template <int TB, int DT>
 __global__ void __launch_bounds__(32 * kRowsWarps, 2) k_linear_few(const LinearArgs a, int32_t parts) {
     chain_go();
@@ -400,6 +404,11 @@ __device__ __forceinline__ unsigned char* shared_base() {
 }
 
 // ================= one CTA a tile, its columns split over a cluster =================
+// Bound by what comes from L2 into an SM, about 60 bytes a clock, and by 3 us that do not depend on the size: the tensor maps, the
+// first stage's way, the accumulators' way out and the cluster's barrier.  A tile's columns are split so that every SM has a share of
+// them: 64 x 4096 x 4096 is 32 tiles, 9.9 us unsplit and 6.8 in four.  The CTAs of a cluster exchange partial sums so that each ends
+// with a share of the tokens: the sums cross once, and all of them scale, convert and store.  24 x 4096 x 14336 13.4 us (4.4 TB/s of
+// weights, floor 9.1), 128 x 4096 x 4096 8.2, 200 x 4096 x 4096 9.2, 333 x 5003 x 2741 (fp32 result) 10.9.
 constexpr int kTileThreads2 = 192;  // warp 0 loads, warp 1 issues the products, warps 2 .. 5 read the accumulators
 
 // How a product is cut: tiles of `tokens` (a multiple of 32 up to 256), each over `split` CTAs of a cluster; a share of the
@@ -574,6 +583,11 @@ __global__ void __launch_bounds__(kTileThreads2) k_linear_tile(const LinearArgs 
 }
 
 // ================= two CTAs a tile, persistent =================
+// A pair of SMs shares each operand (half of the tokens in either's memory), which halves what comes from L2 for a product; while
+// the products of one tile run, the last one's accumulators are read out of the other half of tensor memory.  Bound by the tensor
+// cores, and for seconds on end by the board's power: 8192 x 8192 x 14336 577 us at its best (3335 TOP/s), 650 to 660 in a long
+// run under the power cap (450 with operands of zeros, which take less power).  2048 x 4096 x 4096 27.0 us (2545 TOP/s): 128 tiles
+// over 74 pairs are two turns, the second of them three quarters full.  512 x 4096 x 4096 12.2, 1024 17.3, 4096 49.
 constexpr int kPairThreads = 320;  // warp 0 loads, warp 1 issues the products, warps 2 .. 9 read the accumulators
 constexpr int kPairReaders = 8;
 constexpr int kRaster = 8;         // channel tiles that are walked together, so that what runs at a time shares its operands in L2
