@@ -441,8 +441,8 @@ struct Copier {
     static constexpr int kEach = NV * (int)sizeof(T) / 2;
     const char* row;  // of the next copy; VEC: from this thread's first column on
     int64_t step;     // bytes from row to row
-    __device__ __forceinline__ void init(const void* m, int64_t ld, int64_t r, int64_t teams) {
-        row = static_cast<const char*>(m) + (r * ld + (VEC ? 8 * (int)threadIdx.x : 0)) * (int64_t)sizeof(T);
+    __device__ __forceinline__ void init(const void* m, int64_t ld, int64_t r, int64_t teams, int lead) {
+        row = static_cast<const char*>(m) + (r * ld + (VEC ? 8 * (int)threadIdx.x - lead : 0)) * (int64_t)sizeof(T);
         step = teams * ld * (int64_t)sizeof(T);
     }
     __device__ __forceinline__ void next(uint32_t stage, int cols) {
@@ -502,17 +502,33 @@ __device__ __forceinline__ void staged8(const T* row, const unsigned char* stage
     }
 }
 
+// Columns of the norm's gradient in VEC with LEAD: they count from the 16 bytes in which the team's rows begin, `lead` elements before them,
+// the same in all of its rows and all matrices; so every access but a row's first and last is a vector wherever rows start.
+// (Without LEAD the lead is 0 at compile time: as a variable it cost rows on 16 bytes a third, 8192 x 8192 99.6 -> 133 us.)
+__device__ __forceinline__ void load8_from(const float* row, int lead, int c, int end, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = c + e >= lead && c + e < end ? row[c + e - lead] : 0.0f;
+}
+template <typename T>
+__device__ __forceinline__ void store8_from(T* row, int lead, int c, int end, const float (&v)[8]) {
+    if (c >= lead) return store8<true>(row - lead, c, end, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e >= lead && e < end) narrow(v[e], row[e - lead]);
+}
+
 // A team takes rows in steps of the number of teams.  Its rows pass through `stages` stages of shared memory that asynchronous
 // copies fill ahead, so that what is in flight does not depend on where the team stands between its barriers.  A lane keeps its
 // columns, so the weights and the partial sums of dweight stay in registers, NV pieces of 8.  blockDim: (32 * warps, teams), more
 // than one team only of one warp.
 //   With n = h r, r = 1 / sqrt(mean(h^2) + eps) and s = mean(dy weight n):  dx = r (dy weight - n s) + dh,  dweight = sum dy n.
 // Both sums of a row go through one reduction, so a row costs one pass and one barrier.  Bound by memory where rows start on 16
-// bytes: bf16 8192 x 4096 49.6 us (floor 41), 8192 x 8192 99.6 (82), 4096 x 14336 80.5 (72); what is left is the partial sums' way
-// and the last rows of the teams.  Other rows are read from shared memory an element a lane, and stored so: bound by
-// instructions and the load/store unit, 8192 x 4099 84.5.
-template <int DT, bool VEC, int NV>
-__global__ void __launch_bounds__(32 * backward_warps(NV), NV == 4 ? 1 : 2) k_norm_backward(const NormBackArgs a, int stages, uint32_t row_bytes) {
+// bytes: bf16 8192 x 4096 48.2 us (floor 41), 8192 x 8192 87.4 (82), 4096 x 14336 80.5 (72); what is left is the partial sums' way
+// and the last rows of the teams.  The same with LEAD, whose teams are fewer warps with more columns: 8192 x 4099 63.0.  Rows that
+// start differently in different matrices are read from shared memory an element a lane, and stored so: bound by instructions and the
+// load/store unit, 8192 x 4099 84.5.
+template <int DT, bool VEC, bool LEAD, int NV>
+__global__ void __launch_bounds__(NV == 4 ? 512 : NV == 2 ? 288 : 256, NV == 4 ? 1 : 2) k_norm_backward(const NormBackArgs a, int stages, uint32_t row_bytes) {
     chain_go();
     chain_wait();
     typedef typename Store<DT>::type T;
@@ -527,16 +543,17 @@ __global__ void __launch_bounds__(32 * backward_warps(NV), NV == 4 ? 1 : 2) k_no
     const uint32_t stage_bytes = 3 * row_bytes;
     unsigned char* const first = s_rows + threadIdx.y * stages * stage_bytes;
     unsigned char* const last = first + (stages - 1) * stage_bytes;
+    const int lead = LEAD ? row_shift(static_cast<const T*>(a.h) + me * a.ldh) : 0, end = cols + lead;
     Copier<VEC, NV, T> copy_h, copy_dy, copy_dh;
-    copy_h.init(a.h, a.ldh, me, teams);
-    copy_dy.init(a.dy, a.lddy, me, teams);
-    copy_dh.init(a.dh, a.lddh, me, teams);
+    copy_h.init(a.h, a.ldh, me, teams, lead);
+    copy_dy.init(a.dy, a.lddy, me, teams, lead);
+    copy_dh.init(a.dh, a.lddh, me, teams, lead);
     auto copy = [&](unsigned char* stage, bool there) {
         const uint32_t to = (uint32_t)__cvta_generic_to_shared(stage);
         if (there) {
-            copy_h.next(to, cols);
-            copy_dy.next(to + row_bytes, cols);
-            if (a.dh) copy_dh.next(to + 2 * row_bytes, cols);
+            copy_h.next(to, end);
+            copy_dy.next(to + row_bytes, end);
+            if (a.dh) copy_dh.next(to + 2 * row_bytes, end);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
@@ -546,9 +563,12 @@ __global__ void __launch_bounds__(32 * backward_warps(NV), NV == 4 ? 1 : 2) k_no
     for (int j = 0; j < NV; ++j) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) w[j][e] = 1.0f, sum[j][e] = 0.0f;
-        if (a.weight) load8<VEC>(a.weight, column(j), cols, w[j]);
+        if (a.weight) {
+            if constexpr (LEAD) load8_from(a.weight, lead, column(j), end, w[j]);
+            else load8<VEC>(a.weight, column(j), cols, w[j]);
+        }
     }
-    // where rows start within 16 bytes (all of them the same in VEC: 0)
+    // where rows start within 16 bytes (VEC: the lead)
     const T* h = static_cast<const T*>(a.h) + me * a.ldh;
     const T* dy = static_cast<const T*>(a.dy) + me * a.lddy;
     const T* dh = static_cast<const T*>(a.dh) + me * a.lddh;
@@ -569,8 +589,14 @@ __global__ void __launch_bounds__(32 * backward_warps(NV), NV == 4 ? 1 : 2) k_no
         copy(stage == first ? last : stage - stage_bytes, ahead < a.rows);
         float hv[kHold ? NV : 1][8], gv[kHold ? NV : 1][8], sq = 0.0f, along = 0.0f;
         auto get = [&](int j) {
-            staged8<VEC>(h, stage, column(j), cols, hv[kHold ? j : 0]);
-            staged8<VEC>(dy, stage + row_bytes, column(j), cols, gv[kHold ? j : 0]);
+            const int i = kHold ? j : 0;
+            staged8<VEC>(h, stage, column(j), end, hv[i]);
+            staged8<VEC>(dy, stage + row_bytes, column(j), end, gv[i]);
+            if (LEAD && j == 0 && column(0) < lead) {  // what stands before the row
+#pragma unroll
+                for (int e = 0; e < 7; ++e)
+                    if (e < lead) hv[i][e] = 0.0f, gv[i][e] = 0.0f;
+            }
         };
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -590,14 +616,15 @@ __global__ void __launch_bounds__(32 * backward_warps(NV), NV == 4 ? 1 : 2) k_no
             if (!kHold) get(j);
 #pragma unroll
             for (int e = 0; e < 8; ++e) o[e] = 0.0f;
-            if (a.dh) staged8<VEC>(dh, stage + 2 * row_bytes, column(j), cols, o);
+            if (a.dh) staged8<VEC>(dh, stage + 2 * row_bytes, column(j), end, o);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float g = gv[i][e] * root;
                 o[e] = fmaf(g, w[j][e], fmaf(-coef * root, hv[i][e], o[e]));
                 sum[j][e] = fmaf(g, hv[i][e], sum[j][e]);
             }
-            store8<VEC>(dx, column(j), cols, o);
+            if (LEAD && j == 0) store8_from(dx, lead, column(0), end, o);
+            else store8<VEC>(dx - lead, column(j), end, o);
         }
         dx += step_dx;
         if constexpr (!VEC) h += step_h, dy += step_dy, dh += step_dh;
@@ -611,7 +638,10 @@ __global__ void __launch_bounds__(32 * backward_warps(NV), NV == 4 ? 1 : 2) k_no
         float* all = reinterpret_cast<float*>(s_rows) + threadIdx.y * 256;
         const int lane = threadIdx.x;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) all[(VEC ? 8 * lane : lane) + kStep<VEC> * e] = sum[0][e];
+        for (int e = 0; e < 8; ++e) {
+            const int at = (VEC ? 8 * lane - lead : lane) + kStep<VEC> * e;
+            if (at >= 0) all[at] = sum[0][e];
+        }
         __syncthreads();
         const int c = threadIdx.y * 32 + lane;
         float total = 0.0f;
@@ -619,7 +649,16 @@ __global__ void __launch_bounds__(32 * backward_warps(NV), NV == 4 ? 1 : 2) k_no
         if (c < cols) a.part[blockIdx.x * slice_stride(a.cols) + c] = total;
     } else {
 #pragma unroll
-        for (int j = 0; j < NV; ++j) store8<VEC>(a.part + me * slice_stride(a.cols), column(j), cols, sum[j]);
+        for (int j = 0; j < NV; ++j) {
+            float* part = a.part + me * slice_stride(a.cols);
+            if constexpr (!LEAD) {
+                store8<VEC>(part, column(j), cols, sum[j]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (column(j) + e >= lead && column(j) + e < end) part[column(j) + e - lead] = sum[j][e];
+            }
+        }
     }
 }
 
@@ -802,38 +841,53 @@ dnns_status run_quantize(const QuantArgs& a, int32_t dtype, void* stream) {
 
 // Warps of a team of the norm's gradient: NV = 2 up to 4096 columns, 4 above (fewer warps, but the weights and sums of 8 more
 // columns a lane in registers); 16 warps where 8 do not hold a row.
+// (Widths that put rows off 16 bytes get room for what stands before a row.)
 Shape norm_backward_shape(int64_t cols) {
+    if (cols % 8) cols += 7;
     if (cols <= 256) return row_shape(cols, 1, 1);
     Shape s = row_shape(cols, cols <= 512 * backward_warps(2) ? 2 : cols <= 768 * backward_warps(3) ? 3 : 4, 16);
     s.teams = 1;
     return s;
 }
-// Blocks of an SM at most: about 16 warps of about 112 registers a thread; the workspace is sized for that many, a slice a block.
-int norm_backward_blocks(const Shape& s) { return std::max(1, 18 / (s.warps * s.teams)); }
+// Blocks of an SM at most: 16 warps of 128 registers a thread (NV = 2: 18 of 112); the workspace is sized for that many, a slice a block.
+int norm_backward_blocks(const Shape& s) { return std::max(1, (s.nv == 2 ? 18 : 16) / (s.warps * s.teams)); }
 int64_t norm_backward_slices(int64_t rows, int64_t cols) {
     const Shape s = norm_backward_shape(cols);
     return std::min<int64_t>((rows + s.teams - 1) / s.teams, 148 * norm_backward_blocks(s));
 }
 
-// Launches the gradient; how many slices of partial sums it writes, or -1.
-template <int DT, bool VEC>
-int64_t launch_norm_backward(const NormBackArgs& a, cudaStream_t st) {
-    static std::atomic<uint64_t> done[4];
+template <int DT, bool VEC, bool LEAD>
+auto norm_backward_kernel(int nv) {
+    return nv == 1 ? k_norm_backward<DT, VEC, LEAD, 1> : nv == 2 ? k_norm_backward<DT, VEC, LEAD, 2> : nv == 3 ? k_norm_backward<DT, VEC, LEAD, 3> : k_norm_backward<DT, VEC, LEAD, 4>;
+}
+
+// Where rows start: all (and the weights) on 16 bytes; all matrices' the same way, row by row; anything else.
+enum class Starts { kEven, kShared, kAny };
+// Launches the gradient; how many slices of partial sums it writes, or -1.  Rows of a layer of any width, contiguous in all matrices,
+// are the ordinary case of kShared: 8192 x 4099 takes 63.0 us with their vectors, 84.5 by elements at any place.
+template <int DT>
+int64_t launch_norm_backward(const NormBackArgs& a, Starts starts, cudaStream_t st) {
+    static std::atomic<uint64_t> done[3][4];
     constexpr size_t kRoom = 200 * 1024;  // shared memory of an SM that the stages may take
+    constexpr int kLead = DT == DNNS_F32 ? 3 : 7;
     const Shape s = norm_backward_shape(a.cols);
-    const size_t row_bytes = ((size_t)a.cols * (DT == DNNS_F32 ? 4 : 2) + 15) / 16 * 16 + (VEC ? 0 : 16), stage = 3 * row_bytes * s.teams;
+    const bool vec = starts == Starts::kEven || (starts == Starts::kShared && a.cols + kLead <= (int64_t)256 * s.nv * s.warps);
+    const size_t row_bytes = ((size_t)a.cols * (DT == DNNS_F32 ? 4 : 2) + 15) / 16 * 16 + (starts == Starts::kEven ? 0 : 16), stage = 3 * row_bytes * s.teams;
     int blocks = norm_backward_blocks(s);
-    while (blocks > 1 && kRoom / blocks < 3 * stage) --blocks;
+    // (two blocks of two stages rather than one of three: bf16 8192 x 8192 99.5 -> 87.4 us)
+    while (blocks > 1 && kRoom / blocks < 2 * stage) --blocks;
     const int stages = (int)std::min<size_t>(3, kRoom / blocks / stage);
     if (s.nv == 0 || stages < 2) {
         const int64_t grid = std::min<int64_t>(a.rows, 148);
-        return launch_chained(k_norm_backward_long<DT, VEC>, (unsigned)grid, 512, 0, st, 1, a) ? grid : -1;
+        return launch_chained(starts == Starts::kEven ? k_norm_backward_long<DT, true> : k_norm_backward_long<DT, false>, (unsigned)grid, 512, 0, st, 1, a) ? grid : -1;
     }
-    const int64_t grid = std::min<int64_t>((a.rows + s.teams - 1) / s.teams, 148 * blocks);
+    int64_t grid = std::min<int64_t>((a.rows + s.teams - 1) / s.teams, 148 * blocks);
+    // a team's rows have one lead: it steps over a multiple of 8 rows
+    if (vec && starts == Starts::kShared && grid * s.teams < a.rows) grid -= grid * s.teams % 8 / s.teams;
     const dim3 block(32 * s.warps, s.teams);
-    const auto kernel = s.nv == 1 ? k_norm_backward<DT, VEC, 1> : s.nv == 2 ? k_norm_backward<DT, VEC, 2> : s.nv == 3 ? k_norm_backward<DT, VEC, 3> : k_norm_backward<DT, VEC, 4>;
+    const auto kernel = !vec ? norm_backward_kernel<DT, false, false>(s.nv) : starts == Starts::kEven ? norm_backward_kernel<DT, true, false>(s.nv) : norm_backward_kernel<DT, true, true>(s.nv);
     int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || !allow_shared(kernel, kRoom, done[s.nv - 1], dev)) return -1;
+    if (cudaGetDevice(&dev) != cudaSuccess || !allow_shared(kernel, kRoom, done[!vec ? 0 : starts == Starts::kEven ? 1 : 2][s.nv - 1], dev)) return -1;
     const size_t shared = std::max(stages * stage, s.nv == 1 ? (size_t)kBlockWarps * 256 * sizeof(float) : 0);
     return launch_chained(kernel, (unsigned)grid, block, shared, st, 1, a, stages, (uint32_t)row_bytes) ? grid : -1;
 }
@@ -905,10 +959,11 @@ dnns_status dnns_rmsnorm_backward(const void* dy, int64_t lddy, const void* h, i
         if (ws_bytes < dnns_rmsnorm_backward_workspace_bytes(rows, cols)) return DNNS_ERR_WORKSPACE;
     }
     const NormBackArgs a{dy, h, dh, weight, dx, dweight ? static_cast<float*>(ws_dev) : nullptr, lddy, ldh, lddh, lddx, rows, cols, eps};
-    const bool vec = on_16(dy, lddy, rows, e) && on_16(h, ldh, rows, e) && on_16(dx, lddx, rows, e) && (!dh || on_16(dh, lddh, rows, e)) &&
-                     (!weight || on_16(weight, 0, 1, 4));
-    const int64_t slices = dtype == DNNS_F32 ? (vec ? launch_norm_backward<DNNS_F32, true>(a, st) : launch_norm_backward<DNNS_F32, false>(a, st))
-                                            : (vec ? launch_norm_backward<DNNS_BF16, true>(a, st) : launch_norm_backward<DNNS_BF16, false>(a, st));
+    auto like_h = [&](const void* p, int64_t ld) {
+        return (reinterpret_cast<uintptr_t>(p) - reinterpret_cast<uintptr_t>(h)) % 16 == 0 && (rows <= 1 || (ld - ldh) * (int64_t)e % 16 == 0);
+    };
+    const Starts starts = !like_h(dy, lddy) || !like_h(dx, lddx) || (dh && !like_h(dh, lddh)) ? Starts::kAny : on_16(h, ldh, rows, e) && on_16(weight, 0, 1, 4) ? Starts::kEven : Starts::kShared;
+    const int64_t slices = dtype == DNNS_F32 ? launch_norm_backward<DNNS_F32>(a, starts, st) : launch_norm_backward<DNNS_BF16>(a, starts, st);
     if (slices < 0) return DNNS_ERR_CUDA;
     if (dweight && !launch_chained(k_norm_weight_sum, (unsigned)((cols + 7) / 8), 256, 0, st, 1, a.part, slices, cols, dweight)) return DNNS_ERR_CUDA;
     return cudaGetLastError() == cudaSuccess ? DNNS_OK : DNNS_ERR_CUDA;

@@ -209,6 +209,43 @@ def test_rmsnorm_backward(rows, cols, dtype, kind):
         assert intact(dy, h, dh, dx, dw)
 
 
+@pytest.mark.parametrize("starts", ["shared", "any"])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,cols", [(2500, 5), (2400, 249), (2400, 250), (2400, 256), (900, 505), (901, 512), (310, 4089), (310, 4090), (310, 4097), (300, 5369),
+                                       (300, 5371), (170, 8185), (160, 8186), (150, 16377), (150, 16384)])
+def test_rmsnorm_backward_rows_off_16_bytes(rows, cols, dtype, starts):
+    """Rows that start anywhere, the same way in all matrices or not, around the widths that fill a team's registers; what stands
+    beside them is NaN, and reaches no result.  Rows with an infinity stay by themselves."""
+    g = gen(rows + cols)
+    places = [(3, 3)] * 4 if starts == "shared" else [(3, 3), (0, 1), (5, 7), (1, 1)]   # columns before and between rows
+    def matrix(i, source=None):
+        before, between = places[i]
+        flat = torch.full((before + rows * (cols + between),), float("nan"), device="cuda", dtype=dtype)
+        view = flat[before:].as_strided((rows, cols), (cols + between, 1))
+        if source is not None:
+            view.copy_(source)
+        return flat, view
+    rnd = lambda: torch.randn(rows, cols, generator=g, device="cuda")
+    (_, dy), (_, h), (_, dh) = matrix(0, rnd()), matrix(1, 2 * rnd()), matrix(2, rnd())
+    flat, dx = matrix(3)
+    w = 1 + 0.3 * torch.randn(cols + 1, generator=g, device="cuda")[1:]
+    dw = torch.empty(cols, device="cuda")
+    space = R.rmsnorm_q8_backward_workspace(rows, cols)
+    R.rmsnorm_q8_backward(dy, h, w, 1e-5, dx, dw, dh=dh, workspace=space)
+    ex, size, ew, wsize = norm_gradient(dy.double(), h.double(), w.double(), 1e-5, dh.double())
+    u = P.U32 if dtype is F32 else P.UBF
+    assert torch.all((dx.double() - ex).abs() <= u * ex.abs() + (1 + u) * P.ROW_EPS * size)
+    assert torch.all((dw.double() - ew).abs() <= (P.ROW_EPS + rows * P.U32) * wsize)
+    assert int(flat.isnan().sum()) == flat.numel() - rows * cols                         # written: the rows and nothing else
+    first = dx.clone()
+    row = rows // 2
+    dy[row, cols - 1] = float("inf")
+    R.rmsnorm_q8_backward(dy, h, w, 1e-5, dx, dh=dh)
+    assert not dx[row].isfinite().any()
+    dx[row] = first[row]
+    assert torch.equal(dx, first)
+
+
 @pytest.mark.parametrize("rows,cols", [(3, 33), (40, 520), (2, 4099)])
 def test_rmsnorm_backward_against_differences(rows, cols):
     """<dx, d> + <dweight, e> against the difference quotient of the norm itself (64 bits), and the sum of both for x and
