@@ -306,6 +306,38 @@ def test_silu_gate_backward(rows, cols, dtype, kind):
     assert intact(dy, *bufs)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,cols", [(3, 1), (3, 2), (9, 7), (17, 9), (5, 241), (9, 247), (9, 248), (9, 249), (9, 255), (9, 257), (3, 496), (2, 1985), (5, 5003), (2, 11003)])
+def test_silu_gate_backward_rows_off_16_bytes(rows, cols, dtype):
+    """Every place within 16 bytes at which a row of each matrix may begin, what stands beside the rows NaN; and in place."""
+    g = gen(7 * rows + cols)
+    u = P.U32 if dtype is F32 else P.UBF
+    for turn in range(16):
+        def matrix(i, source=None):
+            before, between = [(0, 0, 0, turn % 8, turn // 2), (1, 3, turn, 2, 5), (turn, 1, 8, 3 * turn, 7), (5, 5, 5, 5, turn), (turn, 0, 1, 2, 3)][turn % 5][i], (turn + (i * turn) % 3) % 9
+            flat = torch.full((before + rows * (cols + between) + 8,), float("nan"), device="cuda", dtype=dtype)
+            view = flat[before:].as_strided((rows, cols), (cols + between, 1))
+            if source is not None:
+                view.copy_(source)
+            return flat, view
+        rnd = lambda s: s * torch.randn(rows, cols, generator=g, device="cuda")
+        (_, dy), (fg, gate), (fu, up) = matrix(0, rnd(1)), matrix(1, rnd(3)), matrix(2, rnd(1))
+        (fdg, dgate), (fdu, dup) = matrix(3), matrix(4)
+        R.silu_gate_q8_backward(dy, gate, up, dgate, dup)
+        d, a, b = dy.double(), gate.double(), up.double()
+        s = 1 / (1 + torch.exp(-a))
+        eg, eu = d * b * s * (1 + a * (1 - s)), d * a * s
+        size = (d * b * s).abs() * (1 + (a * (1 - s)).abs())
+        assert torch.all((dgate.double() - eg).abs() <= u * eg.abs() + (1 + u) * P.ROW_EPS * size)
+        assert torch.all((dup.double() - eu).abs() <= u * eu.abs() + (1 + u) * P.ROW_EPS * eu.abs())
+        for flat in (fdg, fdu):
+            assert int(flat.isnan().sum()) == flat.numel() - rows * cols                  # written: the rows and nothing else
+        R.silu_gate_q8_backward(dy, gate, up, gate, up)
+        assert torch.equal(gate, dgate) and torch.equal(up, dup)
+        for flat in (fg, fu):
+            assert int(flat.isnan().sum()) == flat.numel() - rows * cols
+
+
 def test_silu_gate_backward_against_differences_and_in_place():
     rows, cols = 6, 77
     g = gen(2)
