@@ -523,8 +523,8 @@ __device__ __forceinline__ void store8_from(T* row, int lead, int c, int end, co
 // than one team only of one warp.
 //   With n = h r, r = 1 / sqrt(mean(h^2) + eps) and s = mean(dy weight n):  dx = r (dy weight - n s) + dh,  dweight = sum dy n.
 // Both sums of a row go through one reduction, so a row costs one pass and one barrier.  Bound by memory where rows start on 16
-// bytes: bf16 8192 x 4096 48.2 us (floor 41), 8192 x 8192 87.4 (82), 4096 x 14336 80.5 (72); what is left is the partial sums' way
-// and the last rows of the teams.  The same with LEAD, whose teams are fewer warps with more columns: 8192 x 4099 63.0.  Rows that
+// bytes: bf16 8192 x 4096 46.9 us (floor 41), 8192 x 8192 86.1 (82), 4096 x 14336 81.1 (72); what is left is the partial sums' way
+// and the last rows of the teams.  The same with LEAD, whose teams are fewer warps with more columns: 8192 x 4099 61.8.  Rows that
 // start differently in different matrices are read from shared memory an element a lane, and stored so: bound by instructions and the
 // load/store unit, 8192 x 4099 84.5.
 template <int DT, bool VEC, bool LEAD, int NV>
@@ -720,24 +720,27 @@ __global__ void __launch_bounds__(512) k_norm_backward_long(const NormBackArgs a
     }
 }
 
-// dweight[c] = sum of the teams' partial sums in a fixed order: 8 columns (a sector) by 32 runs of teams a block.
-// Bound by latency (a thread has ten loads or so, eight on their way together): 296 slices of 4096 columns, 4.8 MB, 7.5 us by itself
-// with cold caches, and less behind the kernel that wrote them, from L2.
-__global__ void __launch_bounds__(256) k_norm_weight_sum(const float* part, int64_t teams, int64_t cols, float* dweight) {
+// dweight[c] = sum of the teams' partial sums in a fixed order: 8 columns (a sector) by 32 or 128 runs of teams a block.
+// Bound by latency, so a thread has about ten loads, eight on their way together; narrow rows have many teams, hence the 128:
+// 1328 slices of 1003 columns in 32 runs 19.7 us (cold), in 128 5.9.  296 slices of 4096 columns, 4.8 MB, 7.5 us by itself with cold
+// caches, and less behind the kernel that wrote them, from L2.
+constexpr int kSumRuns = 128;
+__global__ void __launch_bounds__(8 * kSumRuns) k_norm_weight_sum(const float* part, int64_t teams, int64_t cols, float* dweight) {
     chain_go();
     chain_wait();
-    __shared__ float s[32][9];
+    __shared__ float s[kSumRuns][9];
     const int64_t c0 = (int64_t)blockIdx.x * 8;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = threadIdx.x & 7, run = threadIdx.x >> 3;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = threadIdx.x & 7, run = threadIdx.x >> 3, runs = blockDim.x >> 3;
     float sum = 0.0f;
     if (c0 + col < cols) {
 #pragma unroll 8
-        for (int64_t g = run; g < teams; g += 32) sum += part[g * slice_stride(cols) + c0 + col];
+        for (int64_t g = run; g < teams; g += runs) sum += part[g * slice_stride(cols) + c0 + col];
     }
     s[run][col] = sum;
     __syncthreads();
-    if (c0 + warp < cols) {
+    if (warp < 8 && c0 + warp < cols) {
         float all = s[lane][warp];
+        for (int i = lane + 32; i < runs; i += 32) all += s[i][warp];
 #pragma unroll
         for (int d = 16; d; d >>= 1) all += __shfl_xor_sync(kFullMask, all, d);
         if (lane == 0) dweight[c0 + warp] = all;
@@ -864,7 +867,7 @@ auto norm_backward_kernel(int nv) {
 // Where rows start: all (and the weights) on 16 bytes; all matrices' the same way, row by row; anything else.
 enum class Starts { kEven, kShared, kAny };
 // Launches the gradient; how many slices of partial sums it writes, or -1.  Rows of a layer of any width, contiguous in all matrices,
-// are the ordinary case of kShared: 8192 x 4099 takes 63.0 us with their vectors, 84.5 by elements at any place.
+// are the ordinary case of kShared: 8192 x 4099 takes 61.8 us with their vectors, 84.5 by elements at any place.
 template <int DT>
 int64_t launch_norm_backward(const NormBackArgs& a, Starts starts, cudaStream_t st) {
     static std::atomic<uint64_t> done[3][4];
@@ -965,7 +968,7 @@ dnns_status dnns_rmsnorm_backward(const void* dy, int64_t lddy, const void* h, i
     const Starts starts = !like_h(dy, lddy) || !like_h(dx, lddx) || (dh && !like_h(dh, lddh)) ? Starts::kAny : on_16(h, ldh, rows, e) && on_16(weight, 0, 1, 4) ? Starts::kEven : Starts::kShared;
     const int64_t slices = dtype == DNNS_F32 ? launch_norm_backward<DNNS_F32>(a, starts, st) : launch_norm_backward<DNNS_BF16>(a, starts, st);
     if (slices < 0) return DNNS_ERR_CUDA;
-    if (dweight && !launch_chained(k_norm_weight_sum, (unsigned)((cols + 7) / 8), 256, 0, st, 1, a.part, slices, cols, dweight)) return DNNS_ERR_CUDA;
+    if (dweight && !launch_chained(k_norm_weight_sum, (unsigned)((cols + 7) / 8), slices > 320 ? 8 * kSumRuns : 256, 0, st, 1, a.part, slices, cols, dweight)) return DNNS_ERR_CUDA;
     return cudaGetLastError() == cudaSuccess ? DNNS_OK : DNNS_ERR_CUDA;
 }
 
