@@ -722,8 +722,8 @@ __global__ void __launch_bounds__(512) k_norm_backward_long(const NormBackArgs a
 
 // dweight[c] = sum of the teams' partial sums in a fixed order: 8 columns (a sector) by 32 or 128 runs of teams a block.
 // Bound by latency, so a thread has about ten loads, eight on their way together; narrow rows have many teams, hence the 128:
-// 1328 slices of 1003 columns in 32 runs 19.7 us (cold), in 128 5.9.  296 slices of 4096 columns, 4.8 MB, 7.5 us by itself with cold
-// caches, and less behind the kernel that wrote them, from L2.
+// 1328 slices of 1003 columns in 32 runs 19.7 us (cold), in 128 5.9 (gradient of 16384 rows 47.0 -> 36.4).
+// With up to 320 slices 32 runs are the better: the gradient of 8192 x 4096, 296 slices, 46.9 us against 49.5 with 128.
 constexpr int kSumRuns = 128;
 __global__ void __launch_bounds__(8 * kSumRuns) k_norm_weight_sum(const float* part, int64_t teams, int64_t cols, float* dweight) {
     chain_go();
