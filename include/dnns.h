@@ -479,6 +479,7 @@ dnns_status dnns_rmsnorm_quantize(const void* x, int64_t ldx, const void* residu
  * Its gradient at h, rounding passed straight through.  With r = 1 / sqrt(mean(h^2) + eps) and g = dy * weight:
  *   dx = r * (g - h*r * mean(g * h*r)) + dh   (dh nullable: the gradient that reaches h past the norm),
  * which is the gradient of x and of residual alike, and dweight (fp32 [cols], nullable) = sum over rows of dy * h * r.
+ * A row whose sum of squares is not finite in fp32 gets NaN in all of dx and makes dweight NaN, as the norm itself gives it up.
  * dx may be dy, h or dh itself.  ws_dev (16-byte aligned, dnns_rmsnorm_backward_workspace_bytes; only for dweight)
  * receives the partial sums of row groups, which a second kernel adds in a fixed order.  Errors: also WORKSPACE.
  */

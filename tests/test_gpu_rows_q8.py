@@ -246,6 +246,38 @@ def test_rmsnorm_backward_rows_off_16_bytes(rows, cols, dtype, starts):
     assert torch.equal(dx, first)
 
 
+@pytest.mark.parametrize("starts", ["even", "shared", "any"])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,cols", [(300, 64), (300, 1000), (200, 4096), (40, 4099), (9, 8200), (5, 16384), (3, 40000)])
+def test_rmsnorm_backward_of_lost_rows(rows, cols, dtype, starts):
+    """A row whose squares pass fp32 is lost as in the norm itself: its gradient is NaN, and with it the sum over rows, instead of one
+    that looks like a number.  The other rows keep their bits."""
+    if starts == "even":
+        cols = (cols + 7) // 8 * 8
+    g = gen(rows + cols)
+    def matrix(i, scale):
+        before, between = {"even": (0, (-cols) % 8), "shared": (3, 3), "any": [(3, 3), (0, 1), (5, 7), (1, 1)][i]}[starts]
+        flat = torch.zeros(before + rows * (cols + between) + 8, device="cuda", dtype=dtype)
+        view = flat[before:].as_strided((rows, cols), (cols + between, 1))
+        view.copy_(scale * torch.randn(rows, cols, generator=g, device="cuda"))
+        return view
+    dy, h, dh, dx = matrix(0, 1.0), matrix(1, 2.0), matrix(2, 0.5), matrix(3, 1.0)
+    w = 1 + 0.3 * torch.randn(cols, generator=g, device="cuda")
+    dw, space = torch.empty(cols, device="cuda"), R.rmsnorm_q8_backward_workspace(rows, cols)
+    R.rmsnorm_q8_backward(dy, h, w, 1e-5, dx, dw, dh=dh, workspace=space)
+    first = dx.clone()
+    assert first.isfinite().all() and dw.isfinite().all()
+    lost = [0, rows // 2]
+    h[lost[0]] = 1e25
+    h[lost[1], cols // 3] = float("inf")
+    R.rmsnorm_q8_backward(dy, h, w, 1e-5, dx, dw, dh=dh, workspace=space)
+    assert dx[lost].isnan().all() and dw.isnan().all()
+    dx[lost] = first[lost]
+    assert torch.equal(dx, first)
+    forward = R.rmsnorm_q8(h, w, 1e-5, R.RowsQ8(rows, cols))
+    assert forward.scale[lost].isnan().all() and int(forward.scale.isnan().sum()) == len(set(lost))
+
+
 @pytest.mark.parametrize("rows,cols", [(3, 33), (40, 520), (2, 4099)])
 def test_rmsnorm_backward_against_differences(rows, cols):
     """<dx, d> + <dweight, e> against the difference quotient of the norm itself (64 bits), and the sum of both for x and
