@@ -22,14 +22,12 @@ struct Calls {
     decltype(&dnns_linear_quantized) linear_quantized;
 } g_calls = {};
 
-// Rows in 8 bits: the addresses of a RowsQ8's tensors, which it keeps alive.
+// Rows in 8 bits: a RowsQ8's tensors.  Their addresses are taken at each call, since a tensor may be given other storage in between
+// (set_, .data) or lose its own.
 struct Rows {
     PyObject_HEAD
-    int8_t* q;
-    float* scale;
-    uint16_t* values;
-    int64_t ldq, ldv, rows, cols;
-    int64_t device;
+    at::Tensor q, scale, values;  // values: undefined where there are none
+    int64_t rows, cols;
 };
 PyTypeObject RowsType = {PyVarObject_HEAD_INIT(nullptr, 0)};
 
@@ -94,11 +92,37 @@ Rows* rows_of(PyObject* o) {
     if (Py_TYPE(o) != &RowsType) return refuse("rows", "rows in 8 bits", o), nullptr;
     return reinterpret_cast<Rows*>(o);
 }
+// Where the tensors of rows are now.
+struct Place {
+    int8_t* q;
+    float* scale;
+    uint16_t* values;
+    int64_t ldq, ldv;
+};
+// The first rows x cols of a tensor, unit column stride, within its storage.
+bool holds(const at::Tensor& t, int64_t rows, int64_t cols) {
+    if (rows == 0 || cols == 0) return true;
+    return (t.storage_offset() + (rows - 1) * t.stride(0) + cols) * (int64_t)t.itemsize() <= (int64_t)t.storage().nbytes();
+}
 // (after a tensor of the call was found on the current device)
-bool rows_here(const Rows* r) {
-    if (r->device == c10::cuda::current_device()) return true;
-    PyErr_SetString(PyExc_ValueError, "rows: rows of the current CUDA device are needed");
-    return false;
+bool rows_here(const Rows* r, Place* p) {
+    const at::Tensor &q = r->q, &s = r->scale, &v = r->values;
+    if (q.get_device() != c10::cuda::current_device()) {
+        PyErr_SetString(PyExc_ValueError, "rows: rows of the current CUDA device are needed");
+        return false;
+    }
+    if (q.dim() != 2 || q.size(0) != r->rows || q.size(1) < r->cols || (r->cols > 1 && q.stride(1) != 1) || s.dim() != 1 || s.size(0) != r->rows ||
+        (r->rows > 1 && s.stride(0) != 1) || !holds(q, r->rows, r->cols) || !holds(s, r->rows, 1) ||
+        (v.defined() && (v.dim() != 2 || v.size(0) != r->rows || v.size(1) != r->cols || (r->cols > 1 && v.stride(1) != 1) || !holds(v, r->rows, r->cols)))) {
+        PyErr_SetString(PyExc_ValueError, "rows: a tensor of the rows has another shape, or less storage, than when they were made");
+        return false;
+    }
+    p->q = static_cast<int8_t*>(q.data_ptr());
+    p->scale = static_cast<float*>(s.data_ptr());
+    p->values = v.defined() ? static_cast<uint16_t*>(v.data_ptr()) : nullptr;
+    p->ldq = r->rows > 1 ? q.stride(0) : (r->cols + 15) / 16 * 16;
+    p->ldv = v.defined() && r->rows > 1 ? v.stride(0) : r->cols;
+    return true;
 }
 
 void* stream() { return c10::cuda::getCurrentCUDAStream().stream(); }
@@ -121,19 +145,25 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Py_RETURN_NONE;
 }
 
-// rows(q, ldq, scale, values, ldv, rows, cols, device): all integers
+// rows(q, scale, values or None, cols): tensors that RowsQ8 has checked
 PyObject* rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (!count_is(n, 8)) return nullptr;
-    long long v[8];
-    for (int i = 0; i < 8; ++i) {
-        v[i] = PyLong_AsLongLong(a[i]);
-        if (v[i] == -1 && PyErr_Occurred()) return nullptr;
-    }
+    if (!count_is(n, 4)) return nullptr;
+    const at::Tensor *q = tensor_of(a[0]), *scale = tensor_of(a[1]), *values = tensor_of(a[2]);
+    if (!q || !scale || (!values && a[2] != Py_None)) return PyErr_Format(PyExc_TypeError, "tensors are needed");
+    const long long cols = PyLong_AsLongLong(a[3]);
+    if (cols == -1 && PyErr_Occurred()) return nullptr;
     Rows* r = PyObject_New(Rows, &RowsType);
     if (!r) return nullptr;
-    r->q = reinterpret_cast<int8_t*>(v[0]), r->ldq = v[1], r->scale = reinterpret_cast<float*>(v[2]), r->values = reinterpret_cast<uint16_t*>(v[3]);
-    r->ldv = v[4], r->rows = v[5], r->cols = v[6], r->device = v[7];
+    new (&r->q) at::Tensor(*q);
+    new (&r->scale) at::Tensor(*scale);
+    new (&r->values) at::Tensor(values ? *values : at::Tensor());
+    r->rows = q->size(0), r->cols = cols;
     return reinterpret_cast<PyObject*>(r);
+}
+void rows_dealloc(PyObject* o) {
+    Rows* r = reinterpret_cast<Rows*>(o);
+    r->q.~Tensor(), r->scale.~Tensor(), r->values.~Tensor();
+    PyObject_Free(o);
 }
 
 // quantize_rows(x, rows)
@@ -142,9 +172,10 @@ PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
     at::ScalarType type;
     int32_t dtype;
     Matrix x;
-    if (!count_is(n, 2) || !(r = rows_of(a[1])) || !dtype_of(a[0], "x", &type, &dtype) || !matrix(a[0], r->rows, r->cols, type, "x", &x) || !rows_here(r))
+    Place p;
+    if (!count_is(n, 2) || !(r = rows_of(a[1])) || !dtype_of(a[0], "x", &type, &dtype) || !matrix(a[0], r->rows, r->cols, type, "x", &x) || !rows_here(r, &p))
         return nullptr;
-    return status(g_calls.quantize_rows(x.p, x.ld, dtype, r->rows, r->cols, r->q, r->ldq, r->scale, r->values, r->ldv, stream()));
+    return status(g_calls.quantize_rows(x.p, x.ld, dtype, r->rows, r->cols, p.q, p.ldq, p.scale, p.values, p.ldv, stream()));
 }
 
 // rmsnorm(x, weight, eps, rows, residual, h)
@@ -153,14 +184,15 @@ PyObject* rmsnorm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     at::ScalarType type;
     int32_t dtype;
     Matrix x, res, h;
+    Place p;
     float* w;
     if (!count_is(n, 6) || !(r = rows_of(a[3])) || !dtype_of(a[0], "x", &type, &dtype) || !matrix(a[0], r->rows, r->cols, type, "x", &x) ||
         !vector_or_none(a[1], r->cols, "weight", &w) || !matrix_or_none(a[4], r->rows, r->cols, type, "residual", &res) ||
-        !matrix_or_none(a[5], r->rows, r->cols, type, "h", &h) || !rows_here(r))
+        !matrix_or_none(a[5], r->rows, r->cols, type, "h", &h) || !rows_here(r, &p))
         return nullptr;
     const double eps = PyFloat_AsDouble(a[2]);
     if (eps == -1.0 && PyErr_Occurred()) return nullptr;
-    return status(g_calls.rmsnorm_quantize(x.p, x.ld, res.p, res.ld, w, (float)eps, dtype, r->rows, r->cols, h.p, h.ld, r->q, r->ldq, r->scale, r->values, r->ldv,
+    return status(g_calls.rmsnorm_quantize(x.p, x.ld, res.p, res.ld, w, (float)eps, dtype, r->rows, r->cols, h.p, h.ld, p.q, p.ldq, p.scale, p.values, p.ldv,
                                            stream()));
 }
 
@@ -194,10 +226,11 @@ PyObject* silu_gate(PyObject*, PyObject* const* a, Py_ssize_t n) {
     at::ScalarType type;
     int32_t dtype;
     Matrix g, u;
+    Place p;
     if (!count_is(n, 3) || !(r = rows_of(a[2])) || !dtype_of(a[0], "gate", &type, &dtype) || !matrix(a[0], r->rows, r->cols, type, "gate", &g) ||
-        !matrix(a[1], r->rows, r->cols, type, "up", &u) || !rows_here(r))
+        !matrix(a[1], r->rows, r->cols, type, "up", &u) || !rows_here(r, &p))
         return nullptr;
-    return status(g_calls.silu_gate_quantize(g.p, g.ld, u.p, u.ld, dtype, r->rows, r->cols, r->q, r->ldq, r->scale, r->values, r->ldv, stream()));
+    return status(g_calls.silu_gate_quantize(g.p, g.ld, u.p, u.ld, dtype, r->rows, r->cols, p.q, p.ldq, p.scale, p.values, p.ldv, stream()));
 }
 
 // silu_gate_backward(dy, gate, up, dgate, dup)
@@ -219,14 +252,15 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
     at::ScalarType type;
     int32_t dtype;
     Matrix y;
+    Place xp, wp;
     float* bias;
     if (!count_is(n, 5) || !(x = rows_of(a[0])) || !(w = rows_of(a[1])) || !vector_or_none(a[2], w->rows, "bias", &bias) ||
-        !dtype_of(a[3], "y", &type, &dtype) || !matrix(a[3], x->rows, w->rows, type, "y", &y) || !rows_here(x) || !rows_here(w))
+        !dtype_of(a[3], "y", &type, &dtype) || !matrix(a[3], x->rows, w->rows, type, "y", &y) || !rows_here(x, &xp) || !rows_here(w, &wp))
         return nullptr;
     if (x->cols != w->cols) return PyErr_Format(PyExc_ValueError, "x has %lld columns, the layer %lld", (long long)x->cols, (long long)w->cols);
     uint32_t* where = static_cast<uint32_t*>(PyLong_AsVoidPtr(a[4]));
     if (!where && PyErr_Occurred()) return nullptr;
-    return status(g_calls.linear_quantized(x->q, x->ldq, x->scale, w->q, w->ldq, w->scale, bias, x->rows, x->cols, w->rows, dtype, y.p, y.ld, where, stream()));
+    return status(g_calls.linear_quantized(xp.q, xp.ldq, xp.scale, wp.q, wp.ldq, wp.scale, bias, x->rows, x->cols, w->rows, dtype, y.p, y.ld, where, stream()));
 }
 
 // torch reports by exceptions (no device, a tensor without storage): they end here
@@ -252,6 +286,7 @@ PyMODINIT_FUNC PyInit__native() {
     RowsType.tp_name = "_native.Rows";
     RowsType.tp_basicsize = sizeof(Rows);
     RowsType.tp_flags = Py_TPFLAGS_DEFAULT;
+    RowsType.tp_dealloc = rows_dealloc;
     if (PyType_Ready(&RowsType) < 0) return nullptr;
     return PyModule_Create(&module);
 }

@@ -411,7 +411,8 @@ def _row_bytes(cols: int) -> int:
 
 class RowsQ8:
     """A matrix held as rows in 8 bits: ``q`` (int8, rows padded to start on 16 bytes at least), ``scale`` (float32, one a
-    row) and, on request, ``values`` (bfloat16: q * scale)."""
+    row) and, on request, ``values`` (bfloat16: q * scale).  The three tensors stay the same ones; where their memory is,
+    is looked up at each call."""
 
     def __init__(self, rows: int, cols: int, device="cuda:0", values: bool = False):
         self._set(torch.empty(rows, _row_bytes(cols), dtype=torch.int8, device=device),
@@ -434,10 +435,14 @@ class RowsQ8:
         if values is not None and (values.dtype is not torch.bfloat16 or values.shape != (rows, cols) or values.device != q.device
                                    or (cols > 1 and values.stride(1) != 1)):
             raise ValueError(f"values: a {rows} x {cols} bfloat16 matrix beside q is needed, got {tuple(values.shape)} {values.dtype}")
-        self.rows, self.cols, self.q, self.scale, self.values, self.device = rows, cols, q, scale, values, q.device
-        self._c = _native.rows(q.data_ptr(), q.stride(0) if rows > 1 else B.dnns_quantized_row_bytes(cols), scale.data_ptr(),
-                               0 if values is None else values.data_ptr(),
-                               0 if values is None else values.stride(0) if rows > 1 else cols, rows, cols, q.get_device())
+        self.rows, self.cols, self.device = rows, cols, q.device
+        self._q, self._scale, self._values = q, scale, values
+        self._c = _native.rows(q, scale, values, cols)
+
+    # (not to be replaced: _c holds the same tensors)
+    q = property(lambda self: self._q)
+    scale = property(lambda self: self._scale)
+    values = property(lambda self: self._values)
 
 
 def quantize_rows(x: torch.Tensor, out: RowsQ8) -> RowsQ8:
