@@ -5,6 +5,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <ATen/core/grad_mode.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -34,6 +35,7 @@ PyTypeObject RowsType = {PyVarObject_HEAD_INIT(nullptr, 0)};
 struct Matrix {
     void* p = nullptr;
     int64_t ld = 0;
+    const at::Tensor* t = nullptr;
 };
 
 bool refuse(const char* what, const char* wants, PyObject* got) {
@@ -47,6 +49,18 @@ bool on_device(const at::Tensor& t, const char* what) {
     if (t.is_cuda() && t.get_device() == c10::cuda::current_device()) return true;
     PyErr_Format(PyExc_ValueError, "%s: a tensor of the current CUDA device is needed", what);
     return false;
+}
+
+// The calls record nothing for autograd, so a result of a tensor that requires a gradient would be cut off from its graph without a
+// word: it is refused where torch would record.
+bool not_recorded(const at::Tensor& t, const char* what) {
+    if (!t.requires_grad() || !at::GradMode::is_enabled()) return true;
+    PyErr_Format(PyExc_ValueError, "%s: requires a gradient, which the call would not record: call it under torch.no_grad(), or with a detached tensor", what);
+    return false;
+}
+// A tensor was written: torch's check of what was saved for a gradient sees it.  (Tensors of inference mode count no versions.)
+void wrote(const at::Tensor* t) {
+    if (t && t->defined() && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
 }
 
 // dtype of a matrix of fp32 or bf16
@@ -66,7 +80,8 @@ bool matrix(PyObject* o, int64_t rows, int64_t cols, at::ScalarType type, const 
         PyErr_Format(PyExc_ValueError, "%s: a %lld x %lld matrix of the right type with unit column stride is needed", what, (long long)rows, (long long)cols);
         return false;
     }
-    if (!on_device(*t, what)) return false;
+    if (!on_device(*t, what) || !not_recorded(*t, what)) return false;
+    m->t = t;
     m->p = t->data_ptr();
     m->ld = rows > 1 ? t->stride(0) : std::max(cols, t->stride(0));
     return true;
@@ -75,15 +90,17 @@ bool matrix_or_none(PyObject* o, int64_t rows, int64_t cols, at::ScalarType type
     return o == Py_None || matrix(o, rows, cols, type, what, m);
 }
 
-bool vector_or_none(PyObject* o, int64_t n, const char* what, float** p) {
+bool vector_or_none(PyObject* o, int64_t n, const char* what, float** p, const at::Tensor** which = nullptr) {
     *p = nullptr;
+    if (which) *which = nullptr;
     if (o == Py_None) return true;
     const at::Tensor* t = tensor_of(o);
     if (!t || t->scalar_type() != at::kFloat || t->dim() != 1 || t->size(0) != n || !t->is_contiguous()) {
         PyErr_Format(PyExc_ValueError, "%s: a contiguous float32 vector of %lld is needed", what, (long long)n);
         return false;
     }
-    if (!on_device(*t, what)) return false;
+    if (!on_device(*t, what) || !not_recorded(*t, what)) return false;
+    if (which) *which = t;
     *p = static_cast<float*>(t->data_ptr());
     return true;
 }
@@ -117,6 +134,7 @@ bool rows_here(const Rows* r, Place* p) {
         PyErr_SetString(PyExc_ValueError, "rows: a tensor of the rows has another shape, or less storage, than when they were made");
         return false;
     }
+    if (!not_recorded(s, "scale of rows") || (v.defined() && !not_recorded(v, "values of rows"))) return false;
     p->q = static_cast<int8_t*>(q.data_ptr());
     p->scale = static_cast<float*>(s.data_ptr());
     p->values = v.defined() ? static_cast<uint16_t*>(v.data_ptr()) : nullptr;
@@ -133,6 +151,16 @@ bool count_is(Py_ssize_t n, Py_ssize_t want) {
 }
 
 PyObject* status(dnns_status s) { return PyLong_FromLong(s); }
+// The status of a call that wrote rows, or other tensors.
+PyObject* status(dnns_status s, const Rows* r) {
+    if (s == DNNS_OK) wrote(&r->q), wrote(&r->scale), wrote(&r->values);
+    return status(s);
+}
+PyObject* status(dnns_status s, std::initializer_list<const at::Tensor*> written) {
+    if (s == DNNS_OK)
+        for (const at::Tensor* t : written) wrote(t);
+    return status(s);
+}
 
 // bind(addresses in the order of Calls)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -175,7 +203,7 @@ PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Place p;
     if (!count_is(n, 2) || !(r = rows_of(a[1])) || !dtype_of(a[0], "x", &type, &dtype) || !matrix(a[0], r->rows, r->cols, type, "x", &x) || !rows_here(r, &p))
         return nullptr;
-    return status(g_calls.quantize_rows(x.p, x.ld, dtype, r->rows, r->cols, p.q, p.ldq, p.scale, p.values, p.ldv, stream()));
+    return status(g_calls.quantize_rows(x.p, x.ld, dtype, r->rows, r->cols, p.q, p.ldq, p.scale, p.values, p.ldv, stream()), r);
 }
 
 // rmsnorm(x, weight, eps, rows, residual, h)
@@ -192,8 +220,10 @@ PyObject* rmsnorm(PyObject*, PyObject* const* a, Py_ssize_t n) {
         return nullptr;
     const double eps = PyFloat_AsDouble(a[2]);
     if (eps == -1.0 && PyErr_Occurred()) return nullptr;
-    return status(g_calls.rmsnorm_quantize(x.p, x.ld, res.p, res.ld, w, (float)eps, dtype, r->rows, r->cols, h.p, h.ld, p.q, p.ldq, p.scale, p.values, p.ldv,
-                                           stream()));
+    const dnns_status s = g_calls.rmsnorm_quantize(x.p, x.ld, res.p, res.ld, w, (float)eps, dtype, r->rows, r->cols, h.p, h.ld, p.q, p.ldq, p.scale, p.values,
+                                                   p.ldv, stream());
+    if (s == DNNS_OK) wrote(h.t);
+    return status(s, r);
 }
 
 // rmsnorm_backward(dy, h, weight, eps, dx, dweight, dh, workspace)
@@ -204,8 +234,9 @@ PyObject* rmsnorm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int64_t rows = tensor_of(a[1])->size(0), cols = tensor_of(a[1])->size(1);
     Matrix dy, h, dx, dh;
     float *w, *dw;
+    const at::Tensor* dw_t;
     if (!matrix(a[0], rows, cols, type, "dy", &dy) || !matrix(a[1], rows, cols, type, "h", &h) || !vector_or_none(a[2], cols, "weight", &w) ||
-        !matrix(a[4], rows, cols, type, "dx", &dx) || !vector_or_none(a[5], cols, "dweight", &dw) || !matrix_or_none(a[6], rows, cols, type, "dh", &dh))
+        !matrix(a[4], rows, cols, type, "dx", &dx) || !vector_or_none(a[5], cols, "dweight", &dw, &dw_t) || !matrix_or_none(a[6], rows, cols, type, "dh", &dh))
         return nullptr;
     void* ws = nullptr;
     size_t ws_bytes = 0;
@@ -217,7 +248,8 @@ PyObject* rmsnorm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     const double eps = PyFloat_AsDouble(a[3]);
     if (eps == -1.0 && PyErr_Occurred()) return nullptr;
-    return status(g_calls.rmsnorm_backward(dy.p, dy.ld, h.p, h.ld, w, (float)eps, dh.p, dh.ld, dtype, rows, cols, dx.p, dx.ld, dw, ws, ws_bytes, stream()));
+    return status(g_calls.rmsnorm_backward(dy.p, dy.ld, h.p, h.ld, w, (float)eps, dh.p, dh.ld, dtype, rows, cols, dx.p, dx.ld, dw, ws, ws_bytes, stream()),
+                  {dx.t, dw_t});
 }
 
 // silu_gate(gate, up, rows)
@@ -230,7 +262,7 @@ PyObject* silu_gate(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!count_is(n, 3) || !(r = rows_of(a[2])) || !dtype_of(a[0], "gate", &type, &dtype) || !matrix(a[0], r->rows, r->cols, type, "gate", &g) ||
         !matrix(a[1], r->rows, r->cols, type, "up", &u) || !rows_here(r, &p))
         return nullptr;
-    return status(g_calls.silu_gate_quantize(g.p, g.ld, u.p, u.ld, dtype, r->rows, r->cols, p.q, p.ldq, p.scale, p.values, p.ldv, stream()));
+    return status(g_calls.silu_gate_quantize(g.p, g.ld, u.p, u.ld, dtype, r->rows, r->cols, p.q, p.ldq, p.scale, p.values, p.ldv, stream()), r);
 }
 
 // silu_gate_backward(dy, gate, up, dgate, dup)
@@ -243,7 +275,8 @@ PyObject* silu_gate_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Matrix m[5];
     for (int i = 0; i < 5; ++i)
         if (!matrix(a[i], rows, cols, type, names[i], &m[i])) return nullptr;
-    return status(g_calls.silu_gate_backward(m[0].p, m[0].ld, m[1].p, m[1].ld, m[2].p, m[2].ld, dtype, rows, cols, m[3].p, m[3].ld, m[4].p, m[4].ld, stream()));
+    return status(g_calls.silu_gate_backward(m[0].p, m[0].ld, m[1].p, m[1].ld, m[2].p, m[2].ld, dtype, rows, cols, m[3].p, m[3].ld, m[4].p, m[4].ld, stream()),
+                  {m[3].t, m[4].t});
 }
 
 // linear(x rows, weight rows, bias or None, y, status address)
@@ -260,7 +293,8 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (x->cols != w->cols) return PyErr_Format(PyExc_ValueError, "x has %lld columns, the layer %lld", (long long)x->cols, (long long)w->cols);
     uint32_t* where = static_cast<uint32_t*>(PyLong_AsVoidPtr(a[4]));
     if (!where && PyErr_Occurred()) return nullptr;
-    return status(g_calls.linear_quantized(xp.q, xp.ldq, xp.scale, wp.q, wp.ldq, wp.scale, bias, x->rows, x->cols, w->rows, dtype, y.p, y.ld, where, stream()));
+    return status(g_calls.linear_quantized(xp.q, xp.ldq, xp.scale, wp.q, wp.ldq, wp.scale, bias, x->rows, x->cols, w->rows, dtype, y.p, y.ld, where, stream()),
+                  {y.t});
 }
 
 // torch reports by exceptions (no device, a tensor without storage): they end here

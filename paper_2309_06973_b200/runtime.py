@@ -392,6 +392,8 @@ class Deflater:
 
 # ---- variants in 8 bits ------------------------------------------------------------------------------------
 # The calls check their tensors, take the current stream and enter the library in _native (compiled beside it).
+# They record nothing for autograd: tensors that require a gradient are refused where torch would record (use torch.no_grad()), and
+# every write counts as a new version of the tensor.
 from . import _native  # noqa: E402  (after torch, whose libraries it needs)
 
 _native.bind(*(C.cast(getattr(B.lib(), name), C.c_void_p).value for name in (

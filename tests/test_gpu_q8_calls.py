@@ -51,3 +51,74 @@ def test_rows_whose_tensors_lost_their_storage_are_refused():
                          lambda: R.LinearQ8(rows8(8, 512))(rows, y), lambda: R.LinearQ8(rows)(good, torch.empty(4, 4, device="cuda"))):
                 with pytest.raises(ValueError, match="rows: a tensor of the rows"):
                     call()
+
+
+def needs_grad(*shape, dtype=torch.float32):
+    return torch.randn(*shape, device="cuda").to(dtype).requires_grad_()
+
+
+TENSORS = {"quantize_rows": ["x"], "rmsnorm_q8": ["x", "weight", "residual", "h"],
+           "rmsnorm_q8_backward": ["dy", "h", "weight", "dx", "dweight", "dh"], "silu_gate_q8": ["gate", "up"],
+           "silu_gate_q8_backward": ["dy", "gate", "up", "dgate", "dup"], "LinearQ8": ["bias", "y"]}
+
+
+def call_of(name, which):
+    """The call, with that tensor of its own requiring a gradient."""
+    vectors = {"weight": (64,), "dweight": (64,), "bias": (8,), "y": (4, 8)}
+    t = [torch.randn(*vectors.get(n, (4, 64)), device="cuda").requires_grad_(n == which) for n in TENSORS[name]]
+    out, space = R.RowsQ8(4, 64, values=True), R.rmsnorm_q8_backward_workspace(4, 64)
+    return {"quantize_rows": lambda: R.quantize_rows(t[0], out),
+            "rmsnorm_q8": lambda: R.rmsnorm_q8(t[0], t[1], 1e-5, out, residual=t[2], h=t[3]),
+            "rmsnorm_q8_backward": lambda: R.rmsnorm_q8_backward(t[0], t[1], t[2], 1e-5, t[3], t[4], dh=t[5], workspace=space),
+            "silu_gate_q8": lambda: R.silu_gate_q8(t[0], t[1], out),
+            "silu_gate_q8_backward": lambda: R.silu_gate_q8_backward(*t),
+            "LinearQ8": lambda: R.LinearQ8(rows8(8, 64), t[0])(rows8(4, 64), t[1])}[name]
+
+
+@pytest.mark.parametrize("name,which", [(name, which) for name in TENSORS for which in TENSORS[name]])
+def test_a_result_is_not_cut_off_from_a_graph_unsaid(name, which):
+    """The calls record nothing for autograd: a tensor that requires a gradient is refused where it would be recorded, and taken
+    under no_grad and inference_mode."""
+    with pytest.raises(ValueError, match=f"{which}: requires a gradient.*no_grad"):
+        call_of(name, which)()
+    with torch.no_grad():
+        call_of(name, which)()
+    with torch.inference_mode():
+        call_of(name, which)()
+    call_of(name, None)()
+
+
+def test_scales_and_values_that_require_a_gradient():
+    q = torch.zeros(4, 64, dtype=torch.int8, device="cuda")
+    for scale, values in ((needs_grad(4), None), (torch.ones(4, device="cuda"), needs_grad(4, 64, dtype=torch.bfloat16))):
+        rows = R.RowsQ8.of(q, scale, 64, values)
+        with pytest.raises(ValueError, match="no_grad"):
+            R.quantize_rows(torch.randn(4, 64, device="cuda"), rows)
+        with torch.no_grad():
+            R.quantize_rows(torch.randn(4, 64, device="cuda"), rows)
+    with pytest.raises(ValueError, match="no_grad"):
+        R.LinearQ8(rows8(8, 64))(R.RowsQ8.of(q, needs_grad(4), 64), torch.empty(4, 8, device="cuda"))
+
+
+def test_writes_are_counted():
+    """Every output's version goes up, as after any write of torch, so that autograd notices a saved tensor that was overwritten."""
+    new = lambda *s, dtype=torch.float32: torch.randn(*s, device="cuda").to(dtype)
+    out, dx, dw, y, h = R.RowsQ8(4, 64, values=True), new(4, 64), new(64), new(4, 8), new(4, 64)
+    space, layer, dg, du = R.rmsnorm_q8_backward_workspace(4, 64), R.LinearQ8(rows8(8, 64)), new(4, 64), new(4, 64)
+    rows = [out.q, out.scale, out.values]
+    calls = [(lambda: R.quantize_rows(new(4, 64), out), rows),
+             (lambda: R.rmsnorm_q8(new(4, 64), None, 1e-5, out, h=h), rows + [h]),
+             (lambda: R.silu_gate_q8(new(4, 64), new(4, 64), out), rows),
+             (lambda: R.rmsnorm_q8_backward(new(4, 64), new(4, 64), None, 1e-5, dx, dw, workspace=space), [dx, dw]),
+             (lambda: R.silu_gate_q8_backward(new(4, 64), new(4, 64), new(4, 64), dg, du), [dg, du]),
+             (lambda: layer(rows8(4, 64), y), [y])]
+    for call, written in calls:
+        before = [t._version for t in written]
+        call()
+        assert all(t._version > b for t, b in zip(written, before))
+    # the residual stream, saved by an ordinary operator and then updated in place
+    w, res = needs_grad(4, 64), new(4, 64)
+    loss = (w * res).sum()
+    R.rmsnorm_q8(new(4, 64), None, 1e-5, out, residual=res, h=res)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
