@@ -23,12 +23,20 @@ struct Calls {
     decltype(&dnns_linear_quantized) linear_quantized;
 } g_calls = {};
 
+// Where rows in 8 bits are.
+struct Place {
+    int8_t* q;
+    float* scale;
+    uint16_t* values;
+    int64_t ldq, ldv;
+};
 // Rows in 8 bits: a RowsQ8's tensors.  Their addresses are taken at each call, since a tensor may be given other storage in between
-// (set_, .data) or lose its own.
+// (set_, .data) or lose its own.  Or, without tensors, memory that the caller keeps where it is.
 struct Rows {
     PyObject_HEAD
     at::Tensor q, scale, values;  // values: undefined where there are none
-    int64_t rows, cols;
+    Place place;                  // where q is undefined
+    int64_t rows, cols, device;
 };
 PyTypeObject RowsType = {PyVarObject_HEAD_INIT(nullptr, 0)};
 
@@ -109,25 +117,19 @@ Rows* rows_of(PyObject* o) {
     if (Py_TYPE(o) != &RowsType) return refuse("rows", "rows in 8 bits", o), nullptr;
     return reinterpret_cast<Rows*>(o);
 }
-// Where the tensors of rows are now.
-struct Place {
-    int8_t* q;
-    float* scale;
-    uint16_t* values;
-    int64_t ldq, ldv;
-};
 // The first rows x cols of a tensor, unit column stride, within its storage.
 bool holds(const at::Tensor& t, int64_t rows, int64_t cols) {
     if (rows == 0 || cols == 0) return true;
     return (t.storage_offset() + (rows - 1) * t.stride(0) + cols) * (int64_t)t.itemsize() <= (int64_t)t.storage().nbytes();
 }
-// (after a tensor of the call was found on the current device)
+// Where the rows are now (after a tensor of the call was found on the current device).
 bool rows_here(const Rows* r, Place* p) {
     const at::Tensor &q = r->q, &s = r->scale, &v = r->values;
-    if (q.get_device() != c10::cuda::current_device()) {
+    if ((q.defined() ? q.get_device() : r->device) != c10::cuda::current_device()) {
         PyErr_SetString(PyExc_ValueError, "rows: rows of the current CUDA device are needed");
         return false;
     }
+    if (!q.defined()) return *p = r->place, true;
     if (q.dim() != 2 || q.size(0) != r->rows || q.size(1) < r->cols || (r->cols > 1 && q.stride(1) != 1) || s.dim() != 1 || s.size(0) != r->rows ||
         (r->rows > 1 && s.stride(0) != 1) || !holds(q, r->rows, r->cols) || !holds(s, r->rows, 1) ||
         (v.defined() && (v.dim() != 2 || v.size(0) != r->rows || v.size(1) != r->cols || (r->cols > 1 && v.stride(1) != 1) || !holds(v, r->rows, r->cols)))) {
@@ -173,19 +175,30 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Py_RETURN_NONE;
 }
 
-// rows(q, scale, values or None, cols): tensors that RowsQ8 has checked
+// rows(q, scale, values or None, cols): tensors that RowsQ8 has checked; or addresses: rows(q, ldq, scale, values, ldv, rows, cols, device)
 PyObject* rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (!count_is(n, 4)) return nullptr;
-    const at::Tensor *q = tensor_of(a[0]), *scale = tensor_of(a[1]), *values = tensor_of(a[2]);
-    if (!q || !scale || (!values && a[2] != Py_None)) return PyErr_Format(PyExc_TypeError, "tensors are needed");
-    const long long cols = PyLong_AsLongLong(a[3]);
-    if (cols == -1 && PyErr_Occurred()) return nullptr;
+    if (n != 8 && !count_is(n, 4)) return nullptr;
+    const at::Tensor *q = nullptr, *scale = nullptr, *values = nullptr;
+    long long v[8] = {};
+    if (n == 4) {
+        q = tensor_of(a[0]), scale = tensor_of(a[1]), values = tensor_of(a[2]);
+        if (!q || !scale || (!values && a[2] != Py_None)) return PyErr_Format(PyExc_TypeError, "tensors are needed");
+        v[6] = PyLong_AsLongLong(a[3]);
+        if (v[6] == -1 && PyErr_Occurred()) return nullptr;
+        v[5] = q->size(0);
+    } else {
+        for (int i = 0; i < 8; ++i) {
+            v[i] = PyLong_AsLongLong(a[i]);
+            if (v[i] == -1 && PyErr_Occurred()) return nullptr;
+        }
+    }
     Rows* r = PyObject_New(Rows, &RowsType);
     if (!r) return nullptr;
-    new (&r->q) at::Tensor(*q);
-    new (&r->scale) at::Tensor(*scale);
+    new (&r->q) at::Tensor(q ? *q : at::Tensor());
+    new (&r->scale) at::Tensor(scale ? *scale : at::Tensor());
     new (&r->values) at::Tensor(values ? *values : at::Tensor());
-    r->rows = q->size(0), r->cols = cols;
+    r->place = {reinterpret_cast<int8_t*>(v[0]), reinterpret_cast<float*>(v[2]), reinterpret_cast<uint16_t*>(v[3]), v[1], v[4]};
+    r->rows = v[5], r->cols = v[6], r->device = v[7];
     return reinterpret_cast<PyObject*>(r);
 }
 void rows_dealloc(PyObject* o) {

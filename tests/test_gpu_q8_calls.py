@@ -122,3 +122,17 @@ def test_writes_are_counted():
     R.rmsnorm_q8(new(4, 64), None, 1e-5, out, residual=res, h=res)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         loss.backward()
+
+
+def test_rows_at_addresses():
+    """Memory that a program keeps itself, without tensors: the same results."""
+    x, w, y = torch.randn(4, 600, device="cuda"), rows8(8, 600), torch.empty(2, 4, 8, device="cuda")
+    rows, raw = R.quantize_rows(x, R.RowsQ8(4, 600, values=True)), R.RowsQ8(4, 600, values=True)
+    plain = R._native.rows(raw.q.data_ptr(), raw.q.stride(0), raw.scale.data_ptr(), raw.values.data_ptr(), 600, 4, 600, 0)
+    assert R._native.quantize_rows(x, plain) == 0
+    for name in ("q", "scale", "values"):
+        assert torch.equal(getattr(rows, name)[..., :600], getattr(raw, name)[..., :600])
+    layer = R.LinearQ8(w)
+    for r, out in ((rows._c, y[0]), (plain, y[1])):
+        assert R._native.linear(r, w._c, None, out, layer.status.data_ptr()) == 0
+    assert torch.equal(y[0], y[1])
