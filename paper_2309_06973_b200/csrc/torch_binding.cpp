@@ -23,6 +23,15 @@ struct Calls {
     decltype(&dnns_linear_quantized) linear_quantized;
 } g_calls = {};
 
+// A tensor that another one was laid out from, as long as somebody else holds it, and its version then.  (Tensors of inference mode
+// count none.)
+struct Original {
+    c10::weak_intrusive_ptr<c10::TensorImpl, c10::UndefinedTensorImpl> t;
+    int64_t version;
+    static int64_t version_of(c10::TensorImpl* t) { return t->is_inference() ? 0 : (int64_t)t->version_counter().current_version(); }
+    explicit Original(const at::Tensor& from) : t(from.getIntrusivePtr()), version(version_of(from.unsafeGetTensorImpl())) {}
+};
+
 // Where rows in 8 bits are.
 struct Place {
     int8_t* q;
@@ -37,6 +46,7 @@ struct Rows {
     at::Tensor q, scale, values;  // values: undefined where there are none
     Place place;                  // where q is undefined
     int64_t rows, cols, device;
+    Original *of_q, *of_scale;    // null, or the tensors that q and scale were laid out from
 };
 PyTypeObject RowsType = {PyVarObject_HEAD_INIT(nullptr, 0)};
 
@@ -122,6 +132,13 @@ bool holds(const at::Tensor& t, int64_t rows, int64_t cols) {
     if (rows == 0 || cols == 0) return true;
     return (t.storage_offset() + (rows - 1) * t.stride(0) + cols) * (int64_t)t.itemsize() <= (int64_t)t.storage().nbytes();
 }
+// Whether the originals of rows that were laid out anew are both there and have been written since.
+bool changed(const Rows* r) {
+    if (!r->of_q) return false;
+    const auto q = r->of_q->t.lock(), s = r->of_scale->t.lock();
+    return q && s && (Original::version_of(q.get()) != r->of_q->version || Original::version_of(s.get()) != r->of_scale->version);
+}
+
 // Where the rows are now (after a tensor of the call was found on the current device).
 bool rows_here(const Rows* r, Place* p) {
     const at::Tensor &q = r->q, &s = r->scale, &v = r->values;
@@ -199,12 +216,43 @@ PyObject* rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
     new (&r->values) at::Tensor(values ? *values : at::Tensor());
     r->place = {reinterpret_cast<int8_t*>(v[0]), reinterpret_cast<float*>(v[2]), reinterpret_cast<uint16_t*>(v[3]), v[1], v[4]};
     r->rows = v[5], r->cols = v[6], r->device = v[7];
+    r->of_q = r->of_scale = nullptr;
     return reinterpret_cast<PyObject*>(r);
 }
 void rows_dealloc(PyObject* o) {
     Rows* r = reinterpret_cast<Rows*>(o);
+    delete r->of_q;
+    delete r->of_scale;
     r->q.~Tensor(), r->scale.~Tensor(), r->values.~Tensor();
     PyObject_Free(o);
+}
+
+// laid_out(rows, q, scale): the rows were just laid out from these tensors, and follow them
+PyObject* laid_out(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    Rows* r;
+    if (!count_is(n, 3) || !(r = rows_of(a[0]))) return nullptr;
+    const at::Tensor *q = tensor_of(a[1]), *scale = tensor_of(a[2]);
+    if (!q || !scale) return PyErr_Format(PyExc_TypeError, "tensors are needed");
+    auto of_q = std::make_unique<Original>(*q), of_scale = std::make_unique<Original>(*scale);
+    delete r->of_q;
+    delete r->of_scale;
+    r->of_q = of_q.release(), r->of_scale = of_scale.release();
+    Py_RETURN_NONE;
+}
+
+// originals(rows): (q, scale) that the rows follow, or None where they follow none, or nobody holds both any more; changed(rows)
+PyObject* originals(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    Rows* r;
+    if (!count_is(n, 1) || !(r = rows_of(a[0]))) return nullptr;
+    if (!r->of_q) Py_RETURN_NONE;
+    auto q = r->of_q->t.lock(), s = r->of_scale->t.lock();
+    if (!q || !s) Py_RETURN_NONE;
+    return Py_BuildValue("NN", THPVariable_Wrap(at::Tensor(std::move(q))), THPVariable_Wrap(at::Tensor(std::move(s))));
+}
+PyObject* changed(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    Rows* r;
+    if (!count_is(n, 1) || !(r = rows_of(a[0]))) return nullptr;
+    return PyBool_FromLong(changed(r));
 }
 
 // quantize_rows(x, rows)
@@ -292,7 +340,7 @@ PyObject* silu_gate_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
                   {m[3].t, m[4].t});
 }
 
-// linear(x rows, weight rows, bias or None, y, status address)
+// linear(x rows, weight rows, bias or None, y, status address); -1, and nothing done, where the weights' originals were written
 PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Rows *x, *w;
     at::ScalarType type;
@@ -304,6 +352,7 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
         !dtype_of(a[3], "y", &type, &dtype) || !matrix(a[3], x->rows, w->rows, type, "y", &y) || !rows_here(x, &xp) || !rows_here(w, &wp))
         return nullptr;
     if (x->cols != w->cols) return PyErr_Format(PyExc_ValueError, "x has %lld columns, the layer %lld", (long long)x->cols, (long long)w->cols);
+    if (changed(w)) return PyLong_FromLong(-1);
     uint32_t* where = static_cast<uint32_t*>(PyLong_AsVoidPtr(a[4]));
     if (!where && PyErr_Occurred()) return nullptr;
     return status(g_calls.linear_quantized(xp.q, xp.ldq, xp.scale, wp.q, wp.ldq, wp.scale, bias, x->rows, x->cols, w->rows, dtype, y.p, y.ld, where, stream()),
@@ -323,7 +372,7 @@ PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     return nullptr;
 }
 #define DNNS_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<name>)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {DNNS_METHOD(bind),      DNNS_METHOD(rows),      DNNS_METHOD(quantize_rows),      DNNS_METHOD(rmsnorm), DNNS_METHOD(rmsnorm_backward),
+PyMethodDef methods[] = {DNNS_METHOD(bind),      DNNS_METHOD(rows),      DNNS_METHOD(laid_out), DNNS_METHOD(originals), DNNS_METHOD(changed), DNNS_METHOD(quantize_rows),      DNNS_METHOD(rmsnorm), DNNS_METHOD(rmsnorm_backward),
                          DNNS_METHOD(silu_gate), DNNS_METHOD(silu_gate_backward), DNNS_METHOD(linear), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "Calls on rows in 8 bits from torch tensors.", -1, methods};
 

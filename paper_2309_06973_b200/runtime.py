@@ -7,6 +7,7 @@ steps plus read-back helpers.  No step of the method is computed here.
 from __future__ import annotations
 
 import ctypes as C
+import weakref
 from typing import List, Optional
 
 import numpy as np
@@ -440,6 +441,13 @@ class RowsQ8:
         self.rows, self.cols, self.device = rows, cols, q.device
         self._q, self._scale, self._values = q, scale, values
         self._c = _native.rows(q, scale, values, cols)
+        self._layers = ()                       # those that laid these rows out anew
+
+    def _written(self, status: int, where: str) -> "RowsQ8":
+        _done(status, where)
+        for layer in self._layers:
+            layer.refresh()
+        return self
 
     # (not to be replaced: _c holds the same tensors)
     q = property(lambda self: self._q)
@@ -449,15 +457,13 @@ class RowsQ8:
 
 def quantize_rows(x: torch.Tensor, out: RowsQ8) -> RowsQ8:
     """The rows of x in 8 bits: a weight matrix per output channel, or an activation per token."""
-    _done(_native.quantize_rows(x, out._c), "dnns_quantize_rows")
-    return out
+    return out._written(_native.quantize_rows(x, out._c), "dnns_quantize_rows")
 
 
 def rmsnorm_q8(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float, out: RowsQ8,
                residual: Optional[torch.Tensor] = None, h: Optional[torch.Tensor] = None) -> RowsQ8:
     """h = x + residual (stored when given; may be x or residual), out = h * weight / sqrt(mean(h^2) + eps) in 8 bits."""
-    _done(_native.rmsnorm(x, weight, eps, out._c, residual, h), "dnns_rmsnorm_quantize")
-    return out
+    return out._written(_native.rmsnorm(x, weight, eps, out._c, residual, h), "dnns_rmsnorm_quantize")
 
 
 def rmsnorm_q8_backward_workspace(rows: int, cols: int, device="cuda:0") -> torch.Tensor:
@@ -474,8 +480,7 @@ def rmsnorm_q8_backward(dy: torch.Tensor, h: torch.Tensor, weight: Optional[torc
 
 def silu_gate_q8(gate: torch.Tensor, up: torch.Tensor, out: RowsQ8) -> RowsQ8:
     """out = silu(gate) * up in 8 bits."""
-    _done(_native.silu_gate(gate, up, out._c), "dnns_silu_gate_quantize")
-    return out
+    return out._written(_native.silu_gate(gate, up, out._c), "dnns_silu_gate_quantize")
 
 
 def silu_gate_q8_backward(dy: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, dgate: torch.Tensor, dup: torch.Tensor) -> None:
@@ -484,25 +489,59 @@ def silu_gate_q8_backward(dy: torch.Tensor, gate: torch.Tensor, up: torch.Tensor
 
 
 class LinearQ8:
-    """A layer whose weights are rows in 8 bits (a scale per output channel), applied to tokens in 8 bits.  Weights whose
-    rows do not start on 128 bytes are laid out anew, once (products of many tokens then take about a sixth less)."""
+    """A layer whose weights are rows in 8 bits (a scale per output channel), applied to tokens in 8 bits.
+
+    The layer computes with what ``weight`` holds at the time of the call.  Weights whose rows do not start on 128 bytes are laid
+    out anew (products of many tokens then take about a sixth less), and again after each write to them: calls of this module
+    do it themselves, in their own stream; writes of torch to q or scale are seen by their tensors' versions at the layer's next call or
+    use of ``weight``.  What neither shows - a write through a raw address, by the replay of a graph that holds it as an operator of
+    torch, or by torch to tensors of inference mode - takes a ``refresh()``; until then the layer keeps its weights, integers and
+    scales alike."""
 
     def __init__(self, weight: RowsQ8, bias: Optional[torch.Tensor] = None):
         if bias is not None and (bias.dtype is not torch.float32 or bias.shape != (weight.rows,) or not bias.is_contiguous()
                                  or bias.device != weight.device):
             raise ValueError(f"bias: a contiguous float32 vector of {weight.rows} beside the weights is needed, "
                              f"got {tuple(bias.shape)} {bias.dtype}")
-        if weight.rows > 1 and weight.cols > 512 and (weight.q.stride(0) % 128 or weight.q.data_ptr() % 128):
-            q = torch.empty(weight.rows, _row_bytes(weight.cols), dtype=torch.int8, device=weight.device)
-            q[:, : weight.cols] = weight.q[:, : weight.cols]
-            weight = RowsQ8.of(q, weight.scale, weight.cols, weight.values)
-        self.weight, self.bias = weight, bias
-        self.status = torch.zeros(1, dtype=torch.int32, device=weight.device)
-        self._w, self._status_ptr = weight._c, self.status.data_ptr()
+        self._weight, self.bias = weight, bias
+        anew = weight.rows > 1 and weight.cols > 512 and (weight.q.stride(0) % 128 or weight.q.data_ptr() % 128)
+        with torch.inference_mode(False):                  # (tensors made under it could not be written outside)
+            self.status = torch.zeros(1, dtype=torch.int32, device=weight.device)
+            if anew:
+                self._weight = RowsQ8.of(torch.empty(weight.rows, _row_bytes(weight.cols), dtype=torch.int8, device=weight.device),
+                                         torch.empty(weight.rows, dtype=torch.float32, device=weight.device), weight.cols, weight.values)
+        if anew:
+            self._lay_out(weight.q, weight.scale)
+            if not weight._layers:
+                weight._layers = weakref.WeakSet()
+            weight._layers.add(self)
+        self._w, self._status_ptr = self._weight._c, self.status.data_ptr()
+
+    def _lay_out(self, q: torch.Tensor, scale: torch.Tensor) -> None:
+        with torch.no_grad():
+            self._weight.q[:, : self._weight.cols] = q[:, : self._weight.cols]
+            self._weight.scale.copy_(scale)
+        _native.laid_out(self._weight._c, q, scale)
+
+    def refresh(self) -> None:
+        """Lays the weights out anew, where they were, in the current stream."""
+        originals = _native.originals(self._w)
+        if originals is not None:
+            self._lay_out(*originals)
+
+    @property
+    def weight(self) -> RowsQ8:
+        if _native.changed(self._w):
+            self.refresh()
+        return self._weight
 
     def __call__(self, x: RowsQ8, y: torch.Tensor) -> torch.Tensor:
         """y (x.rows, weight.rows) of float32 or bfloat16 = x . weight^T + bias."""
-        _done(_native.linear(x._c, self._w, self.bias, y, self._status_ptr), "dnns_linear_quantized")
+        status = _native.linear(x._c, self._w, self.bias, y, self._status_ptr)
+        if status < 0:                                     # the weights were written
+            self.refresh()
+            status = _native.linear(x._c, self._w, self.bias, y, self._status_ptr)
+        _done(status, "dnns_linear_quantized")
         return y
 
     def device_status(self) -> int:
