@@ -279,9 +279,25 @@ __device__ __forceinline__ uint64_t global_ns() {
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
     return t;
 }
+#ifdef DNNS_BOUNDS_CHECK
+// Checked build only: where set, a wait that does not find its phase complete at once is given up, so that the tests reach what follows.
+__device__ uint32_t g_hurry = 0;
+__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(smem_addr(bar)), "r"(parity) : "memory");
+    return done != 0;
+}
+#endif
 // Wait for a phase of an mbarrier, but not for ever: false when the wait was given up, or another thread of the CTA gave
 // up before.  (The timer takes long to read: it is looked at only after many tries.)
 __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volatile uint32_t* gave_up) {
+#ifdef DNNS_BOUNDS_CHECK
+    if (*(volatile uint32_t*)&g_hurry) {
+        if (mbar_test(bar, parity)) return true;
+        *gave_up = 1;
+        return false;
+    }
+#endif
     if (mbar_try(bar, parity)) return true;
     uint64_t since = 0;
     for (uint32_t spin = 1;; ++spin) {
@@ -295,6 +311,16 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volati
             }
         }
     }
+}
+// The wait for what is in flight when a kernel gives up: it ends by itself, so the limit is only the last resort.
+__device__ __forceinline__ void mbar_drain(uint64_t* bar, uint32_t parity) {
+    const uint64_t since = global_ns();
+    while (!mbar_try(bar, parity) && global_ns() - since < kWaitLimitNs) {
+    }
+}
+// Counts `bytes` at a barrier of this CTA as if a copy had brought them.
+__device__ __forceinline__ void mbar_count(uint64_t* bar, uint32_t bytes) {
+    asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(bar)), "r"(bytes) : "memory");
 }
 // Box of a tensor map into this CTA's shared memory; `bar` counts its bytes (PAIR: may be the pair's first CTA's barrier).
 template <bool PAIR>
@@ -392,7 +418,7 @@ __device__ __forceinline__ void store_columns(const LinearArgs& a, const int32_t
 constexpr int kMaxStages = 10;
 struct TileShared {  // in front of the stages
     uint64_t full[kMaxStages], empty[kMaxStages], done[2], taken[2], drain;
-    uint32_t tmem, gave_up;
+    uint32_t tmem, gave_up, issued[2];  // (pair: stages that the CTAs had copied when they gave up)
     alignas(16) float scales[128];  // of the tokens that a CTA of a cluster stores
 };
 constexpr uint32_t kSharedHead = 2048;
@@ -420,6 +446,17 @@ struct TilePlan {
     __host__ __device__ uint32_t sums_at() const { return kSharedHead + (uint32_t)stages * stage_bytes(); }
     uint32_t shared_bytes() const { return sums_at() + (split > 1 ? (uint32_t)tokens * kTileRows * 4 : 0) + 1024; }
 };
+// Given up, here or in another warp: what is in flight ends before this CTA leaves its memory.  `it`: stages copied (warp 0).  (Not
+// inlined, as pair_gave_up: inside the kernels this code cost calls that never reach it 0.1 to 0.3 us.)
+__device__ __noinline__ void tile_gave_up(TileShared& s, int warp, int lane, int32_t it, int32_t stages, uint32_t* status) {
+    if (lane == 0) {
+        atomicCAS(status, 0u, (uint32_t)DNNS_ERR_TIMEOUT);
+        if (warp == 0)
+            for (int32_t u = max(0, it - stages); u < it; ++u) mbar_drain(&s.full[u % stages], (u / stages) & 1);
+        if (warp == 1) mma_commit<false>(&s.drain), mbar_drain(&s.drain, 0);
+    }
+    __syncwarp();
+}
 template <int DT>
 __global__ void __launch_bounds__(kTileThreads2) k_linear_tile(const LinearArgs a, const __grid_constant__ CUtensorMap wmap,
                                                                const __grid_constant__ CUtensorMap xmap, const TilePlan plan) {
@@ -456,9 +493,10 @@ __global__ void __launch_bounds__(kTileThreads2) k_linear_tile(const LinearArgs 
     const uint32_t tmem = s.tmem;
     volatile uint32_t* gave_up = &s.gave_up;
 
+    int32_t it = 0;  // lane 0 of warps 0 and 1: stages copied, and multiplied
     if (warp == 0) {
         if (lane == 0) {
-            int32_t it = 0, st = 0;
+            int32_t st = 0;
             uint32_t turn = 1;
             for (; it < kbs; ++it) {
                 if (!mbar_wait(&s.empty[st], turn, gave_up)) break;
@@ -468,19 +506,11 @@ __global__ void __launch_bounds__(kTileThreads2) k_linear_tile(const LinearArgs 
                 tile_load<false>(at + kWeightBytes, &xmap, (kb0 + it) * kBlockK, t0, bar);
                 if (++st == plan.stages) st = 0, turn ^= 1;
             }
-            // a wait that was given up: copies in flight are waited for (again with a limit) before the memory is left
-            if (it < kbs) {
-                atomicCAS(a.status, 0u, (uint32_t)DNNS_ERR_TIMEOUT);
-                const uint64_t since = global_ns();
-                for (int32_t u = max(0, it - plan.stages); u < it; ++u)
-                    while (!mbar_try(&s.full[u % plan.stages], (u / plan.stages) & 1) && global_ns() - since < kWaitLimitNs) {
-                    }
-            }
         }
     } else if (warp == 1) {
         if (lane == 0) {
             const uint32_t shape = mma_shape(kTileRows, plan.tokens);
-            int32_t it = 0, st = 0;
+            int32_t st = 0;
             uint32_t turn = 0;
             for (; it < kbs; ++it) {
                 if (!mbar_wait(&s.full[st], turn, gave_up)) break;
@@ -492,15 +522,7 @@ __global__ void __launch_bounds__(kTileThreads2) k_linear_tile(const LinearArgs 
                 mma_commit<false>(&s.empty[st]);
                 if (++st == plan.stages) st = 0, turn ^= 1;
             }
-            if (it == kbs) {
-                mma_commit<false>(&s.done[0]);
-            } else {
-                atomicCAS(a.status, 0u, (uint32_t)DNNS_ERR_TIMEOUT);
-                mma_commit<false>(&s.drain);
-                const uint64_t since = global_ns();
-                while (!mbar_try(&s.drain, 0) && global_ns() - since < kWaitLimitNs) {
-                }
-            }
+            if (it == kbs) mma_commit<false>(&s.done[0]);
         }
     }
     const int quarter = warp & 3;  // tensor memory lanes a warp may read: 32 * (its index mod 4) ..
@@ -509,12 +531,12 @@ __global__ void __launch_bounds__(kTileThreads2) k_linear_tile(const LinearArgs 
     const int share = plan.tokens / split, t1 = t0 + slice * share;  // the tokens that this CTA stores
     if (split > 1)
         for (int i = threadIdx.x; i < share; i += kTileThreads2) s.scales[i] = t1 + i < a.rows ? a.xscale[t1 + i] : 0.0f;
-    // everybody waits for the sums: after this no copy and no product of this CTA is in flight
+    // everybody waits for the sums: once they are there, no copy and no product of this CTA is in flight
     __syncwarp();
     const bool ok = __shfl_sync(kFullMask, (int)(lane == 0 && mbar_wait(&s.done[0], 0, gave_up)), 0);
     mma_fence_after();
     const uint32_t row = tmem + ((uint32_t)(32 * quarter) << 16);
-    if (!ok && threadIdx.x == 64) atomicCAS(a.status, 0u, (uint32_t)DNNS_ERR_TIMEOUT);
+    if (!ok) tile_gave_up(s, warp, lane, it, plan.stages, a.status);
     __syncwarp();
     if (split == 1) {
         if (warp >= 2 && ok) {
@@ -530,7 +552,7 @@ __global__ void __launch_bounds__(kTileThreads2) k_linear_tile(const LinearArgs 
         // in 16 bytes
         const uint32_t sums = smem_addr(base) + plan.sums_at();
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // (the barrier arrived at above)
-        if (warp >= 2) {
+        if (warp >= 2 && ok) {
             int to = 0, slot = slice * (share / 4);  // of the next four columns: the CTA they go to, and their place there
             uint32_t dest = in_cta(sums, 0);
 #pragma unroll 1
@@ -594,6 +616,33 @@ constexpr int kRaster = 8;         // channel tiles that are walked together, so
 
 constexpr uint32_t kPairColumns = 512;  // of tensor memory: two sets of accumulators
 
+__device__ __forceinline__ void tell_pair(uint32_t* where, uint32_t what) {  // both CTAs
+    for (uint32_t r = 0; r < 2; ++r) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(in_cta(smem_addr(where), r)), "r"(what) : "memory");
+}
+// Given up, in either CTA: what is in flight ends before the pair leaves its memory.
+__device__ __noinline__ void pair_gave_up(TileShared& s, uint32_t rank, uint32_t n, uint32_t stage_bytes) {
+    if (threadIdx.x == 0) tell_pair(&s.issued[rank], s.issued[rank]);
+    __syncwarp();
+    __syncthreads();
+    cluster_sync();
+    // The first CTA's barriers count the copies of both; a stage that only one of them had come to is counted full by hand.
+    if (rank == 0 && threadIdx.x == 0) {
+        const uint32_t most = max(s.issued[0], s.issued[1]);
+        for (uint32_t u = most - min(most, n); u < most; ++u) {
+            uint64_t* bar = &s.full[u % n];
+            if (u >= s.issued[0]) mbar_expect(bar, 2 * stage_bytes);
+            if (u >= s.issued[0] || u >= s.issued[1]) mbar_count(bar, stage_bytes);
+            mbar_drain(bar, (u / n) & 1);
+        }
+    }
+    if (threadIdx.x == 32) {  // (behind all that the products' thread had arrive in either CTA)
+        if (rank == 0) mma_commit<true>(&s.drain);
+        mbar_drain(&s.drain, 0);
+    }
+    __syncwarp();
+    __syncthreads();
+    cluster_sync();
+}
 template <int DT>
 __global__ void __launch_bounds__(kPairThreads)
     k_linear_pair(const LinearArgs a, const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, int32_t tokens, int32_t n_stages) {
@@ -658,17 +707,9 @@ __global__ void __launch_bounds__(kPairThreads)
                     if (++st == (uint32_t)n_stages) st = 0, turn ^= 1;
                 }
             }
-            // the products that read this CTA's stages are done once their stages are free again; after a wait that was
-            // given up, copies in flight are waited for (again with a limit)
-            const uint32_t n = min(it, (uint32_t)n_stages);
-            if (!lost) {
-                for (uint32_t u = it - n; u < it && !lost; ++u) lost = !mbar_wait(&s.empty[u % n_stages], (u / n_stages) & 1, gave_up);
-            } else if (rank == 0) {
-                const uint64_t since = global_ns();
-                for (uint32_t u = it - n; u < it; ++u)
-                    while (!mbar_try(&s.full[u % n_stages], (u / n_stages) & 1) && global_ns() - since < kWaitLimitNs) {
-                    }
-            }
+            // the products that read this CTA's stages are done once their stages are free again
+            for (uint32_t u = it - min(it, (uint32_t)n_stages); u < it && !lost; ++u) lost = !mbar_wait(&s.empty[u % n_stages], (u / n_stages) & 1, gave_up);
+            s.issued[rank] = it;
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
@@ -695,12 +736,6 @@ __global__ void __launch_bounds__(kPairThreads)
                     if (++st == (uint32_t)n_stages) st = 0, turn ^= 1;
                 }
                 if (!lost) mma_commit<true>(&s.done[side]);
-            }
-            if (lost) {
-                mma_commit<true>(&s.drain);
-                const uint64_t since = global_ns();
-                while (!mbar_try(&s.drain, 0) && global_ns() - since < kWaitLimitNs) {
-                }
             }
         }
     } else {
@@ -729,11 +764,15 @@ __global__ void __launch_bounds__(kPairThreads)
             if (lane == 0) mbar_arrive_at(in_cta(smem_addr(&s.taken[side]), 0));
         }
     }
-    if (lost) atomicCAS(a.status, 0u, (uint32_t)DNNS_ERR_TIMEOUT);
+    if (lost) {
+        atomicCAS(a.status, 0u, (uint32_t)DNNS_ERR_TIMEOUT);
+        tell_pair(&s.gave_up, 1);
+    }
     __syncwarp();
     mma_fence_before();
     __syncthreads();
-    cluster_sync();  // nothing of the pair is in flight any more
+    cluster_sync();  // unless the pair gave up, nothing of it is in flight any more
+    if (*gave_up) pair_gave_up(s, rank, (uint32_t)n_stages, stage_bytes);
     mma_fence_after();
     if (warp == 1) tmem_free<true>(tmem, kPairColumns);
 }
@@ -927,3 +966,10 @@ extern "C" dnns_status dnns_linear_quantized(const int8_t* xq, int64_t ldx, cons
     const bool launched = dtype == DNNS_F32 ? launch_linear<DNNS_F32>(a, c, n_sm, dev, st) : launch_linear<DNNS_BF16>(a, c, n_sm, dev, st);
     return launched && cudaGetLastError() == cudaSuccess ? DNNS_OK : DNNS_ERR_CUDA;
 }
+
+#ifdef DNNS_BOUNDS_CHECK
+// Checked build only: waits of the product's kernels are given up at once (on the current device) while `on` is not 0.
+extern "C" dnns_status dnns_check_hurry(unsigned int on) {
+    return cudaDeviceSynchronize() == cudaSuccess && cudaMemcpyToSymbol(dnns::g_hurry, &on, sizeof(on)) == cudaSuccess ? DNNS_OK : DNNS_ERR_CUDA;
+}
+#endif
