@@ -392,14 +392,24 @@ class Deflater:
 
 
 # ---- variants in 8 bits ------------------------------------------------------------------------------------
-# The calls check their tensors, take the current stream and enter the library in _native (compiled beside it).
+# The calls check their tensors, take the current stream and enter the library in _native (compiled beside it), which is loaded
+# at the first of them: importing this module loads neither, so that both can still be built.
 # They record nothing for autograd: tensors that require a gradient are refused where torch would record (use torch.no_grad()), and
 # every write counts as a new version of the tensor.
-from . import _native  # noqa: E402  (after torch, whose libraries it needs)
+class _Unloaded:
+    """Stands for _native until something of it is used."""
 
-_native.bind(*(C.cast(getattr(B.lib(), name), C.c_void_p).value for name in (
-    "dnns_quantize_rows", "dnns_rmsnorm_quantize", "dnns_rmsnorm_backward", "dnns_silu_gate_quantize", "dnns_silu_gate_backward",
-    "dnns_linear_quantized")))
+    def __getattr__(self, name):
+        global _native
+        from . import _native as module          # (after torch, whose libraries it needs)
+        module.bind(*(C.cast(getattr(B.lib(), call), C.c_void_p).value for call in (
+            "dnns_quantize_rows", "dnns_rmsnorm_quantize", "dnns_rmsnorm_backward", "dnns_silu_gate_quantize", "dnns_silu_gate_backward",
+            "dnns_linear_quantized")))
+        _native = module
+        return getattr(module, name)
+
+
+_native = _Unloaded()
 
 
 def _done(status: int, where: str):
