@@ -63,8 +63,12 @@ bool refuse(const char* what, const char* wants, PyObject* got) {
 
 const at::Tensor* tensor_of(PyObject* o) { return THPVariable_Check(o) ? &THPVariable_Unpack(o) : nullptr; }
 
+// The current device, asked for once a call (under the interpreter's lock; guarded() forgets it).
+int g_device = -1;
+int device() { return g_device < 0 ? g_device = c10::cuda::current_device() : g_device; }
+
 bool on_device(const at::Tensor& t, const char* what) {
-    if (t.is_cuda() && t.get_device() == c10::cuda::current_device()) return true;
+    if (t.is_cuda() && t.get_device() == device()) return true;
     PyErr_Format(PyExc_ValueError, "%s: a tensor of the current CUDA device is needed", what);
     return false;
 }
@@ -142,7 +146,7 @@ bool changed(const Rows* r) {
 // Where the rows are now (after a tensor of the call was found on the current device).
 bool rows_here(const Rows* r, Place* p) {
     const at::Tensor &q = r->q, &s = r->scale, &v = r->values;
-    if ((q.defined() ? q.get_device() : r->device) != c10::cuda::current_device()) {
+    if ((q.defined() ? q.get_device() : r->device) != device()) {
         PyErr_SetString(PyExc_ValueError, "rows: rows of the current CUDA device are needed");
         return false;
     }
@@ -162,7 +166,7 @@ bool rows_here(const Rows* r, Place* p) {
     return true;
 }
 
-void* stream() { return c10::cuda::getCurrentCUDAStream().stream(); }
+void* stream() { return c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device()).stream(); }
 
 bool count_is(Py_ssize_t n, Py_ssize_t want) {
     if (n != want) PyErr_Format(PyExc_TypeError, "%zd arguments are needed, got %zd", want, n);
@@ -362,6 +366,7 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // torch reports by exceptions (no device, a tensor without storage): they end here
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    g_device = -1;
     try {
         return F(self, a, n);
     } catch (const std::exception& e) {

@@ -453,11 +453,11 @@ class RowsQ8:
         self._c = _native.rows(q, scale, values, cols)
         self._layers = ()                       # those that laid these rows out anew
 
-    def _written(self, status: int, where: str) -> "RowsQ8":
+    def _written(self, status: int, where: str) -> None:
+        """What follows a call that wrote these rows, where it failed or layers laid them out anew."""
         _done(status, where)
         for layer in self._layers:
             layer.refresh()
-        return self
 
     # (not to be replaced: _c holds the same tensors)
     q = property(lambda self: self._q)
@@ -467,13 +467,19 @@ class RowsQ8:
 
 def quantize_rows(x: torch.Tensor, out: RowsQ8) -> RowsQ8:
     """The rows of x in 8 bits: a weight matrix per output channel, or an activation per token."""
-    return out._written(_native.quantize_rows(x, out._c), "dnns_quantize_rows")
+    status = _native.quantize_rows(x, out._c)
+    if status or out._layers:
+        out._written(status, "dnns_quantize_rows")
+    return out
 
 
 def rmsnorm_q8(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float, out: RowsQ8,
                residual: Optional[torch.Tensor] = None, h: Optional[torch.Tensor] = None) -> RowsQ8:
     """h = x + residual (stored when given; may be x or residual), out = h * weight / sqrt(mean(h^2) + eps) in 8 bits."""
-    return out._written(_native.rmsnorm(x, weight, eps, out._c, residual, h), "dnns_rmsnorm_quantize")
+    status = _native.rmsnorm(x, weight, eps, out._c, residual, h)
+    if status or out._layers:
+        out._written(status, "dnns_rmsnorm_quantize")
+    return out
 
 
 def rmsnorm_q8_backward_workspace(rows: int, cols: int, device="cuda:0") -> torch.Tensor:
@@ -490,7 +496,10 @@ def rmsnorm_q8_backward(dy: torch.Tensor, h: torch.Tensor, weight: Optional[torc
 
 def silu_gate_q8(gate: torch.Tensor, up: torch.Tensor, out: RowsQ8) -> RowsQ8:
     """out = silu(gate) * up in 8 bits."""
-    return out._written(_native.silu_gate(gate, up, out._c), "dnns_silu_gate_quantize")
+    status = _native.silu_gate(gate, up, out._c)
+    if status or out._layers:
+        out._written(status, "dnns_silu_gate_quantize")
+    return out
 
 
 def silu_gate_q8_backward(dy: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, dgate: torch.Tensor, dup: torch.Tensor) -> None:
@@ -548,10 +557,11 @@ class LinearQ8:
     def __call__(self, x: RowsQ8, y: torch.Tensor) -> torch.Tensor:
         """y (x.rows, weight.rows) of float32 or bfloat16 = x . weight^T + bias."""
         status = _native.linear(x._c, self._w, self.bias, y, self._status_ptr)
-        if status < 0:                                     # the weights were written
-            self.refresh()
-            status = _native.linear(x._c, self._w, self.bias, y, self._status_ptr)
-        _done(status, "dnns_linear_quantized")
+        if status:
+            if status < 0:                                 # the weights were written
+                self.refresh()
+                status = _native.linear(x._c, self._w, self.bias, y, self._status_ptr)
+            _done(status, "dnns_linear_quantized")
         return y
 
     def device_status(self) -> int:
