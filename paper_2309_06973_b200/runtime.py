@@ -565,7 +565,10 @@ class LinearQ8:
         return y
 
     def device_status(self) -> int:
-        """Synchronises and returns (and clears) the status the layer's kernels recorded."""
+        """Waits for the device, whatever streams the layer ran on, and returns (and clears) the status its kernels recorded."""
+        torch.cuda.synchronize(self.status.device)
         s = int(self.status.item())
-        self.status.zero_()
+        if s:
+            self.status.zero_()
+            torch.cuda.synchronize(self.status.device)     # (before a kernel of another stream records the next)
         return s

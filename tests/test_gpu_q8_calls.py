@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+from paper_2309_06973_b200 import binding as B
 from paper_2309_06973_b200 import runtime as R
 
 pytestmark = pytest.mark.gpu
@@ -136,3 +137,14 @@ def test_rows_at_addresses():
     for r, out in ((rows._c, y[0]), (plain, y[1])):
         assert R._native.linear(r, w._c, None, out, layer.status.data_ptr()) == 0
     assert torch.equal(y[0], y[1])
+
+
+def test_status_of_a_layer_that_ran_on_another_stream():
+    """device_status() waits for whatever stream the layer ran on."""
+    layer, side = R.LinearQ8(rows8(8, 64)), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)
+        layer.status.fill_(B.DNNS_ERR_TIMEOUT)                         # what a kernel of the layer would do there
+    assert layer.device_status() == B.DNNS_ERR_TIMEOUT
+    assert layer.device_status() == B.DNNS_OK
