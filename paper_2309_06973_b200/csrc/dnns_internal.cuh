@@ -320,6 +320,11 @@ struct FoldJob {
 int launch_fold(const Tables& tb, void* arena, const uint64_t* offsets, const int32_t* shapes, uint32_t* job_count,
                 FoldJob* jobs, int n_sm, cudaStream_t st);
 cudaError_t init_kernel_attributes();
+// Whether a call of the CUDA runtime succeeded; its error is taken from the thread, so that only the call that met it reports it.
+inline bool succeeded(cudaError_t e) {
+    if (e != cudaSuccess) (void)cudaGetLastError();
+    return e == cudaSuccess;
+}
 // Launch of a kernel that may begin before the kernel in front of it in the stream has ended: it has chain_wait() before its first
 // access to global memory, so only its set-up (and the launch itself) overlaps, and chain_go() to let the next one do the same.
 // Small kernels in a row cost 0.5 to 1 us less each (a token's norm 3.0 -> 2.5, a small product 5.3 -> 4.1).  Every thread of such a
@@ -335,7 +340,7 @@ inline bool launch_chained(void (*kernel)(P...), dim3 grid, dim3 block, size_t s
     at[1].id = cudaLaunchAttributeClusterDimension;
     at[1].val.clusterDim.x = cluster, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
     cfg.attrs = at, cfg.numAttrs = cluster > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, P(args)...) == cudaSuccess;
+    return succeeded(cudaLaunchKernelEx(&cfg, kernel, P(args)...));
 }
 #ifdef __CUDACC__
 __device__ __forceinline__ void chain_go() { asm volatile("griddepcontrol.launch_dependents;"); }
@@ -346,7 +351,7 @@ template <typename F>
 inline bool allow_shared(F* kernel, size_t bytes, std::atomic<uint64_t>& done, int dev) {
     const uint64_t bit = 1ull << (dev & 63);
     if (dev < 64 && (done.load(std::memory_order_relaxed) & bit)) return true;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return false;
+    if (!succeeded(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes))) return false;
     if (dev < 64) done.fetch_or(bit, std::memory_order_relaxed);
     return true;
 }

@@ -785,7 +785,7 @@ EncodeTiled encode_tiled() {
     static const EncodeTiled fn = [] {
         void* p = nullptr;
         cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        if (!succeeded(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found)) ||
             found != cudaDriverEntryPointSuccess)
             p = nullptr;
         return reinterpret_cast<EncodeTiled>(p);
@@ -960,11 +960,11 @@ extern "C" dnns_status dnns_linear_quantized(const int8_t* xq, int64_t ldx, cons
     if (ldy > span / rows || (in_cols && (ldx > span / rows || ldw > span / out_cols))) return DNNS_ERR_UNSUPPORTED;
     const LinearArgs a{xq, wq, xscale, wscale, bias, y, status_dev, ldx, ldw, ldy, (int32_t)rows, (int32_t)in_cols, (int32_t)out_cols};
     int dev = 0, n_sm = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return DNNS_ERR_CUDA;
+    if (!succeeded(cudaGetDevice(&dev)) || !succeeded(cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev))) return DNNS_ERR_CUDA;
     const Choice c = choose(a, n_sm);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool launched = dtype == DNNS_F32 ? launch_linear<DNNS_F32>(a, c, n_sm, dev, st) : launch_linear<DNNS_BF16>(a, c, n_sm, dev, st);
-    return launched && cudaGetLastError() == cudaSuccess ? DNNS_OK : DNNS_ERR_CUDA;
+    return launched ? DNNS_OK : DNNS_ERR_CUDA;
 }
 
 #ifdef DNNS_BOUNDS_CHECK

@@ -805,7 +805,7 @@ size_t elem_bytes(int32_t dtype) { return dtype == DNNS_F32 ? 4 : 2; }
 
 int sm_count() {
     int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    if (!succeeded(cudaGetDevice(&dev)) || !succeeded(cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev))) return 0;
     return n;
 }
 
@@ -838,7 +838,7 @@ dnns_status run_quantize(const QuantArgs& a, int32_t dtype, void* stream) {
     const dnns_status s = check_quantize(a, dtype, &launch);
     if (s != DNNS_OK || !launch) return s;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (a.cols == 0) return cudaMemsetAsync(a.scale, 0, (size_t)a.rows * sizeof(float), st) == cudaSuccess ? DNNS_OK : DNNS_ERR_CUDA;
+    if (a.cols == 0) return succeeded(cudaMemsetAsync(a.scale, 0, (size_t)a.rows * sizeof(float), st)) ? DNNS_OK : DNNS_ERR_CUDA;
     const int n_sm = sm_count();
     if (n_sm == 0) return DNNS_ERR_CUDA;
     const size_t e = elem_bytes(dtype);
@@ -846,7 +846,7 @@ dnns_status run_quantize(const QuantArgs& a, int32_t dtype, void* stream) {
                      (!a.values || on_16(a.values, a.ldv, a.rows, 2)) && (!a.weight || on_16(a.weight, 0, 1, 4));
     const bool launched = dtype == DNNS_F32 ? (vec ? launch_quantize<OP, DNNS_F32, true>(a, n_sm, st) : launch_quantize<OP, DNNS_F32, false>(a, n_sm, st))
                                             : (vec ? launch_quantize<OP, DNNS_BF16, true>(a, n_sm, st) : launch_quantize<OP, DNNS_BF16, false>(a, n_sm, st));
-    return launched && cudaGetLastError() == cudaSuccess ? DNNS_OK : DNNS_ERR_CUDA;
+    return launched ? DNNS_OK : DNNS_ERR_CUDA;
 }
 
 // Warps of a team of the norm's gradient: NV = 2 up to 4096 columns, 4 above (fewer warps, but the weights and sums of 8 more
@@ -897,7 +897,7 @@ int64_t launch_norm_backward(const NormBackArgs& a, Starts starts, cudaStream_t 
     const dim3 block(32 * s.warps, s.teams);
     const auto kernel = !vec ? norm_backward_kernel<DT, false, false>(s.nv) : starts == Starts::kEven ? norm_backward_kernel<DT, true, false>(s.nv) : norm_backward_kernel<DT, true, true>(s.nv);
     int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || !allow_shared(kernel, kRoom, done[!vec ? 0 : starts == Starts::kEven ? 1 : 2][s.nv - 1], dev)) return -1;
+    if (!succeeded(cudaGetDevice(&dev)) || !allow_shared(kernel, kRoom, done[!vec ? 0 : starts == Starts::kEven ? 1 : 2][s.nv - 1], dev)) return -1;
     const size_t shared = std::max(stages * stage, s.nv == 1 ? (size_t)kBlockWarps * 256 * sizeof(float) : 0);
     return launch_chained(kernel, (unsigned)grid, block, shared, st, 1, a, stages, (uint32_t)row_bytes) ? grid : -1;
 }
@@ -957,7 +957,7 @@ dnns_status dnns_rmsnorm_backward(const void* dy, int64_t lddy, const void* h, i
     if (cols == 0) return DNNS_OK;
     if (reinterpret_cast<uintptr_t>(dweight) % 4 || reinterpret_cast<uintptr_t>(weight) % 4) return DNNS_ERR_INVALID_ARG;
     if (rows == 0) {
-        if (dweight && cudaMemsetAsync(dweight, 0, (size_t)cols * sizeof(float), st) != cudaSuccess) return DNNS_ERR_CUDA;
+        if (dweight && !succeeded(cudaMemsetAsync(dweight, 0, (size_t)cols * sizeof(float), st))) return DNNS_ERR_CUDA;
         return DNNS_OK;
     }
     if (!matrix_arg_ok(dy, lddy, cols, e) || !matrix_arg_ok(h, ldh, cols, e) || !matrix_arg_ok(dx, lddx, cols, e) ||
@@ -976,7 +976,7 @@ dnns_status dnns_rmsnorm_backward(const void* dy, int64_t lddy, const void* h, i
     const int64_t slices = dtype == DNNS_F32 ? launch_norm_backward<DNNS_F32>(a, starts, st) : launch_norm_backward<DNNS_BF16>(a, starts, st);
     if (slices < 0) return DNNS_ERR_CUDA;
     if (dweight && !launch_chained(k_norm_weight_sum, (unsigned)((cols + 7) / 8), slices > 320 ? 8 * kSumRuns : 256, 0, st, 1, a.part, slices, cols, dweight)) return DNNS_ERR_CUDA;
-    return cudaGetLastError() == cudaSuccess ? DNNS_OK : DNNS_ERR_CUDA;
+    return DNNS_OK;
 }
 
 dnns_status dnns_silu_gate_backward(const void* dy, int64_t lddy, const void* gate, int64_t ldg, const void* up, int64_t ldu,
@@ -998,7 +998,7 @@ dnns_status dnns_silu_gate_backward(const void* dy, int64_t lddy, const void* ga
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool launched = dtype == DNNS_F32 ? (vec ? launch_gate_backward<DNNS_F32, true>(a, st) : launch_gate_backward<DNNS_F32, false>(a, st))
                                             : (vec ? launch_gate_backward<DNNS_BF16, true>(a, st) : launch_gate_backward<DNNS_BF16, false>(a, st));
-    return launched && cudaGetLastError() == cudaSuccess ? DNNS_OK : DNNS_ERR_CUDA;
+    return launched ? DNNS_OK : DNNS_ERR_CUDA;
 }
 
 }  // extern "C"

@@ -1,4 +1,6 @@
 """What the calls on rows in 8 bits promise beside their results."""
+import ctypes as C
+
 import pytest
 import torch
 
@@ -148,3 +150,31 @@ def test_status_of_a_layer_that_ran_on_another_stream():
         layer.status.fill_(B.DNNS_ERR_TIMEOUT)                         # what a kernel of the layer would do there
     assert layer.device_status() == B.DNNS_ERR_TIMEOUT
     assert layer.device_status() == B.DNNS_OK
+
+
+def test_an_error_is_reported_by_its_own_call_only():
+    """A launch that CUDA refuses (on the legacy stream while a stream that waits for it is captured) fails its call; the next one,
+    which runs, does not report it again."""
+    cuda = C.CDLL("libcuda.so.1")
+    torch.cuda.synchronize()
+    x, out, w, h = torch.randn(4, 64, device="cuda"), rows8(4, 64), rows8(8, 64), torch.randn(4, 64, device="cuda")
+    y, dw, status = torch.empty(4, 8, device="cuda"), torch.empty(64, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    space = R.rmsnorm_q8_backward_workspace(4, 64)
+    L, p = B.lib(), lambda t: t.data_ptr()
+    calls = [lambda: L.dnns_quantize_rows(p(x), 64, 0, 4, 64, p(out.q), 64, p(out.scale), None, 0, None),
+             lambda: L.dnns_rmsnorm_backward(p(x), 64, p(h), 64, None, 1e-5, None, 0, 0, 4, 64, p(x), 64, p(dw), p(space), space.numel(), None),
+             lambda: L.dnns_silu_gate_backward(p(x), 64, p(h), 64, p(h), 64, 0, 4, 64, p(x), 64, p(h), 64, None),
+             lambda: L.dnns_linear_quantized(p(out.q), 64, p(out.scale), p(w.q), 64, p(w.scale), None, 4, 64, 8, 0, p(y), 8, p(status), None)]
+    torch.cuda.synchronize()
+    for call in calls:
+        stream, graph = C.c_void_p(), C.c_void_p()
+        assert cuda.cuStreamCreate(C.byref(stream), 0) == 0            # a stream that waits for the legacy one
+        assert cuda.cuStreamBeginCapture_v2(stream, 2) == 0            # (relaxed: other calls of this thread stay allowed)
+        refused = call()
+        cuda.cuStreamEndCapture(stream, C.byref(graph))
+        if graph.value:
+            cuda.cuGraphDestroy(graph)
+        assert cuda.cuStreamDestroy_v2(stream) == 0
+        assert refused == B.DNNS_ERR_CUDA
+        assert call() == B.DNNS_OK
+    torch.cuda.synchronize()
