@@ -2,7 +2,7 @@
 // The sum is exact in int32 (at most 2^17 - 1 products of at most 2^14 each), so any order and any split of it gives
 // the same bits.
 //
-// Four kernels, chosen by the number of tokens and the work there is for the SMs (choose() below):
+// Four kernels, chosen by the number of tokens and the work there is for the SMs (choose() below), and one for no columns:
 //   k_linear_rows   one token: bound by reading the weights once; int8 dot products in the ordinary pipes
 //   k_linear_few    up to 32 tokens: the same, with warp-wide products
 //   k_linear_tile   one CTA a tile of 128 channels by up to 256 tokens; the columns of a tile may be split over the CTAs of a
@@ -63,14 +63,15 @@ __device__ __forceinline__ int4 stream16(const int8_t* p) {
 __device__ __forceinline__ int4 token16(const int8_t* p) { return *reinterpret_cast<const int4*>(p); }
 __device__ __forceinline__ int32_t dot16(const int4& a, const int4& b, int32_t c) { return __dp4a(a.x, b.x, __dp4a(a.y, b.y, __dp4a(a.z, b.z, __dp4a(a.w, b.w, c)))); }
 
-// M tokens at most (a.rows of them), blockIdx.y the token group.
+// M tokens at most (a.rows of them), blockIdx.y the token group.  Launched for one token: with two and more, k_linear_few or a tile reads
+// the weights no more often and multiplies faster.
 // 1 x 4096 x 4096 (tokens, columns, channels): 3.0 us with the weights in L2, 4.6 with them in HBM (floor 2.6, and 1.7 of that time is
 // what any kernel of this size takes); 1 x 4096 x 14336 11.2 (5.2 TB/s, floor 9.0); 1 x 1024 x 1024 1.8.
 template <int M, int R, int DT>
 __global__ void __launch_bounds__(32 * kRowsWarps) k_linear_rows(const LinearArgs a, int32_t parts) {
     chain_go();
     chain_wait();
-    constexpr int U = M <= 4 ? 4 : 2;  // loads deep
+    constexpr int U = 4;  // loads deep
     __shared__ int32_t s_part[kRowsWarps][R * M];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int group = warp / parts, part = warp - group * parts;
@@ -145,6 +146,16 @@ __global__ void __launch_bounds__(32 * kRowsWarps) k_linear_rows(const LinearArg
         if (q < kSums && n < a.n && t < a.rows)
             store_out<DT>(a.y, (int64_t)t * a.ldy + n, scaled(mine[b], a.xscale[t], a.wscale[n], a.bias ? a.bias[n] : 0.0f));
     }
+}
+
+// No columns: all sums are 0.  (Not a copy of the bias: a scale that is NaN still gives NaN.)
+template <int DT>
+__global__ void __launch_bounds__(256) k_linear_empty(const LinearArgs a) {
+    chain_go();
+    chain_wait();
+    const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (n >= a.n) return;
+    for (int64_t t = blockIdx.y; t < a.rows; t += gridDim.y) store_out<DT>(a.y, t * a.ldy + n, scaled(0, a.xscale[t], a.wscale[n], a.bias ? a.bias[n] : 0.0f));
 }
 
 // ================= a few more tokens: warp-wide products =================
@@ -837,29 +848,20 @@ bool launch_pair(const LinearArgs& a, int tokens, int n_sm, int dev, cudaStream_
     return launch_chained(k_linear_pair<DT>, grid, kPairThreads, kSharedHead + stages * stage + 1024, st, 2, a, wmap, xmap, (int32_t)tokens, (int32_t)stages);
 }
 
-template <int M, int DT>
-bool launch_rows_of(const LinearArgs& a, int n_sm, cudaStream_t st) {
+template <int DT>
+bool launch_rows(const LinearArgs& a, int n_sm, cudaStream_t st) {
     // two channels a warp where that still leaves a dozen warps an SM (each then has more loads on their way); warps share a
     // channel, down to four loads a lane of each, until there are enough blocks for the SMs to finish together
     const bool two = a.n >= 24 * n_sm;
     int parts = 1;
     while (parts < kRowsWarps && (int64_t)a.n * parts < 6 * (two ? 2 : 1) * kRowsWarps * (int64_t)n_sm && a.k >= 4 * 512 * 2 * parts) parts *= 2;
-    const int64_t step = kRowsWarps / parts * (two ? 2 : 1), most = 65535 * (int64_t)M;  // (the grid's second extent)
-    for (int64_t t0 = 0; t0 < a.rows; t0 += most) {
-        LinearArgs part = a;
-        part.rows = (int32_t)std::min<int64_t>(a.rows - t0, most);
-        part.xq += t0 * a.ldx, part.xscale += t0;
-        part.y = static_cast<char*>(a.y) + t0 * a.ldy * (DT == DNNS_F32 ? 4 : 2);
-        const dim3 grid((unsigned)((a.n + step - 1) / step), (unsigned)((part.rows + M - 1) / M));
-        if (!launch_chained(two ? k_linear_rows<M, 2, DT> : k_linear_rows<M, 1, DT>, grid, 32 * kRowsWarps, 0, st, 1, part, parts)) return false;
-    }
-    return true;
+    const int64_t step = kRowsWarps / parts * (two ? 2 : 1);
+    return launch_chained(two ? k_linear_rows<1, 2, DT> : k_linear_rows<1, 1, DT>, (unsigned)((a.n + step - 1) / step), 32 * kRowsWarps, 0, st, 1, a, parts);
 }
 
 template <int DT>
-bool launch_rows(const LinearArgs& a, int n_sm, cudaStream_t st) {
-    if (a.rows <= 1) return launch_rows_of<1, DT>(a, n_sm, st);
-    return a.rows <= 2 ? launch_rows_of<2, DT>(a, n_sm, st) : launch_rows_of<4, DT>(a, n_sm, st);
+bool launch_empty(const LinearArgs& a, cudaStream_t st) {
+    return launch_chained(k_linear_empty<DT>, dim3((unsigned)(((int64_t)a.n + 255) / 256), (unsigned)std::min(a.rows, 65535)), 256, 0, st, 1, a);
 }
 
 // Warps that share the columns of 16 channels: as long as the 16 warps an SM that fit at a time are not passed (17 x 3000 x 5000 in
@@ -896,7 +898,7 @@ struct Choice {
 //   - k_linear_few pays for each 8 tokens in warp-wide products: 16 x 4096 x 4096 5.9 against 7.4 in tiles, 24 x 4096 x 14336 19.9
 //     against 13.4; and for loads one after the other where the columns are not whole batches: 5 x 700 x 3000 4.4 against 3.7.
 Choice choose(const LinearArgs& a, int n_sm) {
-    if (a.k == 0 || a.rows <= 1) return {0, 0, 1};
+    if (a.rows <= 1) return {0, 0, 1};
     const double bytes = (double)a.n * a.k, memory = bytes / 3400.0;  // 6.5 TB/s
     const double blocks = (a.k + kBlockK - 1) / kBlockK, rough_w = a.ldw % 128 ? 1.2 : 1.0, rough_x = a.ldx % 128 ? 1.2 : 1.0;
     Choice best{8, 0, 1};
@@ -961,8 +963,9 @@ extern "C" dnns_status dnns_linear_quantized(const int8_t* xq, int64_t ldx, cons
     const LinearArgs a{xq, wq, xscale, wscale, bias, y, status_dev, ldx, ldw, ldy, (int32_t)rows, (int32_t)in_cols, (int32_t)out_cols};
     int dev = 0, n_sm = 0;
     if (!succeeded(cudaGetDevice(&dev)) || !succeeded(cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev))) return DNNS_ERR_CUDA;
-    const Choice c = choose(a, n_sm);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (in_cols == 0) return (dtype == DNNS_F32 ? launch_empty<DNNS_F32>(a, st) : launch_empty<DNNS_BF16>(a, st)) ? DNNS_OK : DNNS_ERR_CUDA;
+    const Choice c = choose(a, n_sm);
     const bool launched = dtype == DNNS_F32 ? launch_linear<DNNS_F32>(a, c, n_sm, dev, st) : launch_linear<DNNS_BF16>(a, c, n_sm, dev, st);
     return launched ? DNNS_OK : DNNS_ERR_CUDA;
 }

@@ -587,8 +587,7 @@ __global__ void __launch_bounds__(NV == 4 ? 512 : NV == 2 ? 288 : 256, NV == 4 ?
         // the row is there: this thread's copies and, past the barrier, everybody's; past it the stage before is free, too.  (VEC: a
         // thread reads what it copied itself, and needs neither.)
         if (stages == 2) asm volatile("cp.async.wait_group 0;" ::: "memory");
-        else if (stages == 3) asm volatile("cp.async.wait_group 1;" ::: "memory");
-        else asm volatile("cp.async.wait_group 2;" ::: "memory");
+        else asm volatile("cp.async.wait_group 1;" ::: "memory");
         if constexpr (!VEC) {
             if (warps == 1) __syncwarp();
             else __syncthreads();

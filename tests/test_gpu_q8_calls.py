@@ -178,3 +178,73 @@ def test_an_error_is_reported_by_its_own_call_only():
         assert refused == B.DNNS_ERR_CUDA
         assert call() == B.DNNS_OK
     torch.cuda.synchronize()
+
+
+def test_the_binding_makes_the_same_calls():
+    """binding.py's functions on device addresses against the calls from torch tensors, bit for bit, and their errors."""
+    rows, cols, out_cols = 5, 600, 72
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    x, res, dh = (torch.randn(rows, cols, generator=g, device="cuda").bfloat16() for _ in range(3))
+    w, bias = torch.randn(cols, generator=g, device="cuda"), torch.randn(out_cols, generator=g, device="cuda")
+    layer = R.LinearQ8(R.quantize_rows(torch.randn(out_cols, cols, generator=g, device="cuda"), R.RowsQ8(out_cols, cols)), bias)
+    space, p = R.rmsnorm_q8_backward_workspace(rows, cols), lambda t: t.data_ptr()
+    assert space.numel() == B.dnns_rmsnorm_backward_workspace_bytes(rows, cols) and B.dnns_quantized_row_bytes(cols) == 608
+    a, b = R.RowsQ8(rows, cols, values=True), R.RowsQ8(rows, cols, values=True)
+    ld, stream = a.q.stride(0), torch.cuda.current_stream().cuda_stream
+    new = lambda: [torch.zeros(rows, cols, device="cuda", dtype=torch.bfloat16) for _ in range(2)]
+
+    def same(*pairs):
+        for r in (a, b):
+            pairs += ((r.q[:, :cols].clone(), r.scale.clone(), r.values.clone()),)
+        for u, v in list(pairs[:-2]) + list(zip(*pairs[-2:])):
+            assert torch.equal(u, v)
+
+    R.quantize_rows(x, a)
+    B.dnns_quantize_rows(p(x), cols, B.DNNS_BF16, rows, cols, p(b.q), ld, p(b.scale), p(b.values), cols, stream)
+    same()
+    R.silu_gate_q8(x, res, a)
+    B.dnns_silu_gate_quantize(p(x), cols, p(res), cols, B.DNNS_BF16, rows, cols, p(b.q), ld, p(b.scale), p(b.values), cols, stream)
+    same()
+    h1, h2 = new()
+    R.rmsnorm_q8(x, w, 1e-5, a, residual=res, h=h1)
+    B.dnns_rmsnorm_quantize(p(x), cols, p(res), cols, p(w), 1e-5, B.DNNS_BF16, rows, cols, p(h2), cols, p(b.q), ld, p(b.scale), p(b.values), cols, stream)
+    same((h1, h2))
+    (d1, d2), (w1, w2) = new(), (torch.empty_like(w), torch.empty_like(w))
+    R.rmsnorm_q8_backward(x, h1, w, 1e-5, d1, w1, dh=dh, workspace=space)
+    B.dnns_rmsnorm_backward(p(x), cols, p(h1), cols, p(w), 1e-5, p(dh), cols, B.DNNS_BF16, rows, cols, p(d2), cols, p(w2), p(space), space.numel(), stream)
+    same((d1, d2), (w1, w2))
+    (g1, g2), (u1, u2) = new(), new()
+    R.silu_gate_q8_backward(dh, x, res, g1, u1)
+    B.dnns_silu_gate_backward(p(dh), cols, p(x), cols, p(res), cols, B.DNNS_BF16, rows, cols, p(g2), cols, p(u2), cols, stream)
+    same((g1, g2), (u1, u2))
+    y1, y2 = torch.empty(rows, out_cols, device="cuda"), torch.empty(rows, out_cols, device="cuda")
+    layer(a, y1)
+    B.dnns_linear_quantized(p(a.q), ld, p(a.scale), p(layer.weight.q), ld, p(layer.weight.scale), p(bias), rows, cols, out_cols, B.DNNS_F32, p(y2), out_cols,
+                            p(layer.status), stream)
+    same((y1, y2))
+    for bad in (lambda: B.dnns_quantize_rows(p(x), cols - 1, B.DNNS_BF16, rows, cols, p(b.q), ld, p(b.scale)),
+                lambda: B.dnns_rmsnorm_quantize(p(x), cols, 0, 0, 0, 0.0, B.DNNS_BF16, rows, cols, 0, 0, p(b.q), ld, p(b.scale)),
+                lambda: B.dnns_rmsnorm_backward(p(x), cols, p(h1), cols, 0, 1e-5, 0, 0, B.DNNS_BF16, rows, cols, p(d2), cols, p(w2), p(space), 16),
+                lambda: B.dnns_silu_gate_quantize(p(x), cols, 0, cols, B.DNNS_BF16, rows, cols, p(b.q), ld, p(b.scale)),
+                lambda: B.dnns_silu_gate_backward(p(dh), cols, p(x), cols, p(res), cols, 7, rows, cols, p(g2), cols, p(u2), cols),
+                lambda: B.dnns_linear_quantized(p(a.q), ld, p(a.scale), p(layer.weight.q), ld, p(layer.weight.scale), 0, rows, cols, out_cols, B.DNNS_F32, p(y2),
+                                                out_cols, 0)):
+        with pytest.raises(B.DnnsError):
+            bad()
+
+
+@pytest.mark.parametrize("rows,n", [(1, 1), (1, 3000), (3, 257), (70000, 5)])
+def test_products_of_no_columns(rows, n):
+    """The bias alone, but a NaN scale is still seen, in its row and in its channel; rows of y apart."""
+    for dtype in (torch.float32, torch.bfloat16):
+        xs, ws, bias = torch.ones(rows, device="cuda"), torch.ones(n, device="cuda"), torch.randn(n, device="cuda")
+        x, w = (R.RowsQ8.of(torch.zeros(len(s), 16, dtype=torch.int8, device="cuda"), s, 0) for s in (xs, ws))
+        flat = torch.full((rows * (n + 3),), 7.0, device="cuda", dtype=dtype)
+        y = flat.as_strided((rows, n), (n + 3, 1))
+        R.LinearQ8(w, bias)(x, y)
+        assert torch.equal(y, bias.to(dtype).expand(rows, n))
+        xs[rows - 1] = ws[n // 2] = float("nan")
+        R.LinearQ8(w, bias)(x, y)
+        assert y[rows - 1].isnan().all() and y[:, n // 2].isnan().all() and int(y.isnan().sum()) == rows + n - 1
+        assert bool((flat.as_strided((rows, 3), (n + 3, 1), n) == 7).all())
