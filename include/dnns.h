@@ -450,13 +450,14 @@ dnns_status dnns_inflate(const void* stream_dev, size_t stream_bytes, const uint
  * Common rules
  *   - Matrices of element type dtype (DNNS_F32 / DNNS_BF16) are row-major with unit column stride; ld* counts
  *     elements from row to row and is at least the number of columns (rows may be pieces of wider ones).  Pointers need
- *     the alignment of their element only; rows that start on 16 bytes are fastest.
+ *     the alignment of their element only; rows that start on 16 bytes are fastest.  The norm's gradient reads, and drops, the
+ *     bytes between the 16-byte boundary in front of a row and the row (never past its end).
  *   - Arithmetic, sums and scales are fp32 (the product's sums are exact int32), rounded once where a result is stored.
  *     No call uses atomics on floating point: the same inputs give the same bits.
  *   - Outputs do not overlap inputs, except where a call says so.  rows == 0 does nothing (a gradient that is a sum over
  *     rows is then zero); cols == 0 gives scale 0 for every row.
- *   - Errors: INVALID_ARG (null or misaligned pointer, negative size, an ld below its columns, eps), UNSUPPORTED
- *     (dtype; more than 2^31 - 1 rows or 2^30 columns; a matrix of 2^62 bytes or more), CUDA.
+ *   - Errors come back from the call that met them, and only from it.  INVALID_ARG (null or misaligned pointer, negative size,
+ *     an ld below its columns, eps), UNSUPPORTED (dtype; more than 2^31 - 1 rows or 2^30 columns; a matrix of 2^62 bytes or more), CUDA.
  */
 size_t dnns_quantized_row_bytes(size_t cols); /* cols rounded up to a multiple of 16 */
 
@@ -469,6 +470,7 @@ dnns_status dnns_quantize_rows(const void* x, int64_t ldx, int32_t dtype, int64_
  * Root-mean-square norm with the residual's addition, in 8 bits:
  *   h = x + residual (residual nullable: h = x),   y = h * weight / sqrt(mean(h^2) + eps)  (weight fp32, nullable: 1)
  *   q, scale, values = Q(y);   h_out (nullable, dtype) = h.
+ * y is that of the fp32 sum; only h_out is rounded to dtype.  (The gradient below is that at the h it is given: with bf16, a rounding away.)
  * h_out may be x or residual itself (same pointer and ld): the residual stream updated in place.  eps is at least 2^-126.
  * A row whose sum of squares is not finite in fp32 counts as one with an Inf.
  */
@@ -479,6 +481,7 @@ dnns_status dnns_rmsnorm_quantize(const void* x, int64_t ldx, const void* residu
  * Its gradient at h, rounding passed straight through.  With r = 1 / sqrt(mean(h^2) + eps) and g = dy * weight:
  *   dx = r * (g - h*r * mean(g * h*r)) + dh   (dh nullable: the gradient that reaches h past the norm),
  * which is the gradient of x and of residual alike, and dweight (fp32 [cols], nullable) = sum over rows of dy * h * r.
+ * Its products stay in range where |g| / (mean(h^2) + eps) is below 2^127.
  * A row whose sum of squares is not finite in fp32 gets NaN in all of dx and makes dweight NaN, as the norm itself gives it up.
  * dx may be dy, h or dh itself.  ws_dev (16-byte aligned, dnns_rmsnorm_backward_workspace_bytes; only for dweight)
  * receives the partial sums of row groups, which a second kernel adds in a fixed order.  Errors: also WORKSPACE.
@@ -492,7 +495,8 @@ dnns_status dnns_rmsnorm_backward(const void* dy, int64_t lddy, const void* h, i
  * The gated activation between the products of a block, in 8 bits:  Q(silu(gate) * up),  silu(g) = g / (1 + exp(-g)).
  * gate and up are often the halves of one product's rows.  The gradient (rounding passed straight through), with
  * s = 1 / (1 + exp(-gate)):  dgate = dy * up * s * (1 + gate * (1 - s)),  dup = dy * gate * s.
- * dgate and dup may be dy, gate or up themselves (same pointer and ld).
+ * dgate and dup may be dy, gate or up themselves (same pointer and ld).  s has a relative error of at most (2 |gate| + 12) * 2^-24, and is 0
+ * for gates below -87.3.
  */
 dnns_status dnns_silu_gate_quantize(const void* gate, int64_t ldg, const void* up, int64_t ldu, int32_t dtype, int64_t rows,
                               int64_t cols, int8_t* q, int64_t ldq, float* scale, uint16_t* values, int64_t ldv, void* stream);
@@ -504,7 +508,8 @@ dnns_status dnns_silu_gate_backward(const void* dy, int64_t lddy, const void* ga
  * Product of rows in 8 bits:  y[t][n] = (sum_k xq[t][k] * wq[n][k]) * xscale[t] * wscale[n] + bias[n]
  * for rows tokens, in_cols columns and out_cols output channels (UNSUPPORTED: more than 2^30 tokens or channels); y has
  * element type dtype, rows of ldy elements; bias
- * (fp32, nullable).  The sum is exact: in_cols is at most DNNS_LINEAR_MAX_IN (UNSUPPORTED above), so that int32 holds it.
+ * (fp32, nullable); the factors are multiplied in this order, in fp32.  The sum is exact: in_cols is at most
+ * DNNS_LINEAR_MAX_IN (UNSUPPORTED above), so that int32 holds it.
  * in_cols == 0 leaves the bias.  Every wait of the kernels is bounded; one that runs out ends the kernel, leaves y
  * incomplete and sets *status_dev (device word, cleared by the caller) to DNNS_ERR_TIMEOUT.
  */

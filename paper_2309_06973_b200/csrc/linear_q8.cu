@@ -443,9 +443,9 @@ __device__ __forceinline__ unsigned char* shared_base() {
 // ================= one CTA a tile, its columns split over a cluster =================
 // Bound by what comes from L2 into an SM, about 60 bytes a clock, and by 3 us that do not depend on the size: the tensor maps, the
 // first stage's way, the accumulators' way out and the cluster's barrier.  A tile's columns are split so that every SM has a share of
-// them: 64 x 4096 x 4096 is 32 tiles, 9.9 us unsplit and 6.8 in four.  The CTAs of a cluster exchange partial sums so that each ends
-// with a share of the tokens: the sums cross once, and all of them scale, convert and store.  24 x 4096 x 14336 13.4 us (4.4 TB/s of
-// weights, floor 9.1), 128 x 4096 x 4096 8.2, 200 x 4096 x 4096 9.2, 333 x 5003 x 2741 (fp32 result) 10.9.
+// them: 64 x 4096 x 4096 is 32 tiles, 9.9 us unsplit and 7.6 in four.  The CTAs of a cluster exchange partial sums so that each ends
+// with a share of the tokens: the sums cross once, and all of them scale, convert and store.  24 x 4096 x 14336 13.7 us (4.3 TB/s of
+// weights, floor 9.1; 112 of the SMs have a tile), 128 x 4096 x 4096 8.3, 200 x 4096 x 4096 9.3, 333 x 5003 x 2741 (fp32 result) 11.0.
 constexpr int kTileThreads2 = 192;  // warp 0 loads, warp 1 issues the products, warps 2 .. 5 read the accumulators
 
 // How a product is cut: tiles of `tokens` (a multiple of 32 up to 256), each over `split` CTAs of a cluster; a share of the
@@ -618,7 +618,7 @@ __global__ void __launch_bounds__(kTileThreads2) k_linear_tile(const LinearArgs 
 // ================= two CTAs a tile, persistent =================
 // A pair of SMs shares each operand (half of the tokens in either's memory), which halves what comes from L2 for a product; while
 // the products of one tile run, the last one's accumulators are read out of the other half of tensor memory.  Bound by the tensor
-// cores, and for seconds on end by the board's power: 8192 x 8192 x 14336 577 us at its best (3335 TOP/s), 650 to 660 in a long
+// cores, and for seconds on end by the board's power: 8192 x 8192 x 14336 577 us at its best (3335 TOP/s), 650 to 677 in a long
 // run under the power cap (450 with operands of zeros, which take less power).  2048 x 4096 x 4096 27.0 us (2545 TOP/s): 128 tiles
 // over 74 pairs are two turns, the second of them three quarters full.  512 x 4096 x 4096 12.2, 1024 17.3, 4096 49.
 constexpr int kPairThreads = 320;  // warp 0 loads, warp 1 issues the products, warps 2 .. 9 read the accumulators
@@ -818,7 +818,9 @@ constexpr uint32_t kSharedLimit = 227 * 1024;
 
 TilePlan tile_plan(int32_t rows, int tokens, int split) {
     TilePlan plan{tokens, (rows + tokens - 1) / tokens, split, kMaxStages};
-    const uint32_t room = tokens <= 64 ? kSharedLimit / 2 - 1024 : kSharedLimit;  // small tiles leave room for two CTAs an SM
+    // Small tiles leave room for two CTAs an SM, whether or not the grid has two: where it has not, they go without half of their stages (64
+    // x 4096 x 4096 in four 7.6 us; a tile of 96 tokens, with all of them, took 6.8).
+    const uint32_t room = tokens <= 64 ? kSharedLimit / 2 - 1024 : kSharedLimit;
     while (plan.stages > 2 && plan.shared_bytes() > room) --plan.stages;
     return plan;
 }
@@ -894,7 +896,7 @@ struct Choice {
 //     (k_linear_pair, all SMs at once); rows that do not start on 128 bytes cost more: 333 x 5003 x 2741 (tokens, columns, channels) at a row
 //     distance of 5008 14.2, of 5120 11.3.  Hence large tiles for many tokens (2048 x 4096 x 4096: a pair with 256 tokens 27.0, with
 //     128 39.8), and hence splits, which put every SM to work where there are few tiles (64 x 4096 x 4096: one CTA a tile 9.9,
-//     its columns over four 6.8).  With few stages a stage costs its way from L2 to the product and back instead.
+//     its columns over four 7.6).  With few stages a stage costs its way from L2 to the product and back instead.
 //   - k_linear_few pays for each 8 tokens in warp-wide products: 16 x 4096 x 4096 5.9 against 7.4 in tiles, 24 x 4096 x 14336 19.9
 //     against 13.4; and for loads one after the other where the columns are not whole batches: 5 x 700 x 3000 4.4 against 3.7.
 Choice choose(const LinearArgs& a, int n_sm) {

@@ -2,7 +2,7 @@
 // root-mean-square norm with the residual's addition, and the gated activation - and the gradients of those two.
 //   Q(y): a = max |y|, scale = a / 127, q = rint(y * 127 / a).
 //
-// All five are bound by memory: a few operations an element against 5 to 11 bytes of traffic.  So each row is read
+// All five are bound by memory: a few operations an element against 3 to 10 bytes of traffic in bf16, 5 to 20 in fp32.  So each row is read
 // once and kept in registers (fp32) between the reduction that its scale needs and the stores.  For the norm the
 // reduction is a single one, because q does not depend on the row's root mean square: with v = h * weight and
 // r = 1 / sqrt(mean(h^2) + eps), q = rint(v * 127 / max|v|) and scale = r * max|v| / 127, so the sum of squares and the
@@ -234,8 +234,9 @@ struct QuantArgs {
     float eps;
 };
 
-// 1 / (1 + exp(-g)) to a few units of the last place.  Below g = -87.3, where 1 + exp(-g) passes 2^126, it is 0 (the sigmoid
-// is under 2^-125 there).
+// 1 / (1 + exp(-g)), off by a relative (2 |g| + 12) * 2^-24 at most: -g log2(e) is rounded before its power of two is taken, which is
+// a relative error of |g| * 2^-24, and the constant's rounding another; the rest are the approximations and the sum.  That is under 2^-16,
+// far below what bf16 or 8 bits resolve.  Below g = -87.3, where 1 + exp(-g) passes 2^126, it is 0 (the sigmoid is under 2^-125 there).
 __device__ __forceinline__ float sigmoid(float g) {
     float e, s;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(g * -1.4426950408889634f));
@@ -289,10 +290,10 @@ __device__ __forceinline__ void store_quantized(const QuantArgs& a, int64_t r, i
 
 // Quantisation, of a matrix (OP rows), of h * weight behind the norm, or of silu(gate) * up.  Bound by memory where rows start on 16
 // bytes: one pass, nothing but its inputs and outputs crosses HBM.  Measured (bf16, us; bandwidth of the bytes the call cannot do
-// without): norm 16384 x 8192 with h written 179.5 (6.7 TB/s, as a plain copy), 16384 x 4096 93; gate 8192 x 14336 123.6 (6.65
-// TB/s, gate and up read as the halves of one matrix); rows 14336 x 4096 45.  Other rows are bound by the load/store unit, which
-// takes an element a lane: fp32 2741 x 5003 19.1 (floor 14.7).  One token is bound by the latency of one block: norm 1 x 4096 2.1,
-// gate 1 x 14336 3.3.
+// without): norm 16384 x 8192 with h written 180.5 (6.7 TB/s, as a plain copy); gate 8192 x 14336 124 (6.6 TB/s, gate and up read as
+// the halves of one matrix; 130 and more after some tens of milliseconds under load); rows 14336 x 4096 45.  Other rows are bound by the
+// load/store unit, which takes an element a lane: fp32 rows 2741 x 5003 19.2 (floor 14.7), bf16 rows 14336 x 4099 61 (45), gate 8192 x 5003
+// 65 (44), norm 4096 x 4099 42 (23).  One token is bound by the latency of one block: norm 1 x 4096 2.4, gate 1 x 14336 3.6.
 // blockDim: (32 * warps of a team, teams); more than one team only of one warp
 template <int OP, int DT, bool VEC, int NV>
 __global__ void __launch_bounds__(32 * quantize_warps(NV)) k_rows_quantize(const QuantArgs a) {
@@ -530,7 +531,7 @@ __device__ __forceinline__ float inverse_root(float sq, float inv_n, float eps) 
 // than one team only of one warp.
 //   With n = h r, r = 1 / sqrt(mean(h^2) + eps) and s = mean(dy weight n):  dx = r (dy weight - n s) + dh,  dweight = sum dy n.
 // Both sums of a row go through one reduction, so a row costs one pass and one barrier.  Bound by memory where rows start on 16
-// bytes: bf16 8192 x 4096 46.9 us (floor 41), 8192 x 8192 86.1 (82), 4096 x 14336 81.1 (72); what is left is the partial sums' way
+// bytes: bf16 8192 x 4096 47.2 us (floor 41), 8192 x 8192 87.3 (82), 4096 x 14336 82.5 (72), fp32 8192 x 4096 94 (82); what is left is the partial sums' way
 // and the last rows of the teams.  The same with LEAD, whose teams are fewer warps with more columns: 8192 x 4099 61.8.  Rows that
 // start differently in different matrices are read from shared memory an element a lane, and stored so: bound by instructions and the
 // load/store unit, 8192 x 4099 84.5.
@@ -668,9 +669,10 @@ __global__ void __launch_bounds__(NV == 4 ? 512 : NV == 2 ? 288 : 256, NV == 4 ?
     }
 }
 
-// The same for rows that do not fit in shared memory: walked twice, the partial sums in the team's slice of the workspace.  Bound by
-// that second walk and by the sums' way (a read and a write an element): fp32 1024 x 40000 280 us (floor 100).  Norms of this width
-// are rare, so it stays the plain loop that it is.
+// The same for rows of which two stages of three matrices do not fit in shared memory (fp32 from about 8530 columns on), or whose columns do
+// not fit in a team's registers (16384): walked twice, the partial sums in the team's slice of the workspace.  Bound by that second
+// walk and by the sums' way (a read and a write an element), and so 2.5 to 2.8 times the floor: fp32 4096 x 12288 310 us (floor 123),
+// 4096 x 14336 389 (144), 1024 x 40000 280 (100).
 template <int DT, bool VEC>
 __global__ void __launch_bounds__(512) k_norm_backward_long(const NormBackArgs a) {
     chain_go();
@@ -848,8 +850,8 @@ dnns_status run_quantize(const QuantArgs& a, int32_t dtype, void* stream) {
     return launched ? DNNS_OK : DNNS_ERR_CUDA;
 }
 
-// Warps of a team of the norm's gradient: NV = 2 up to 4096 columns, 4 above (fewer warps, but the weights and sums of 8 more
-// columns a lane in registers); 16 warps where 8 do not hold a row.
+// Warps of a team of the norm's gradient: NV = 2 up to 4096 columns, 3 up to 6144, 4 above (fewer warps, but the weights and sums of 8
+// more columns a lane in registers); 16 warps where 8 do not hold a row.
 // (Widths that put rows off 16 bytes get room for what stands before a row.)
 Shape norm_backward_shape(int64_t cols) {
     if (cols % 8) cols += 7;
@@ -858,11 +860,14 @@ Shape norm_backward_shape(int64_t cols) {
     s.teams = 1;
     return s;
 }
-// Blocks of an SM at most: 16 warps of 128 registers a thread (NV = 2: 18 of 112); the workspace is sized for that many, a slice a block.
+// Blocks of an SM at most: 16 warps of 128 registers a thread.  NV = 2 is built for 96 and gets 18 warps (three teams of six, where 4096
+// columns take two of eight); that spills 4 to 84 bytes a thread but for bf16 on 16 bytes.  The workspace is sized for that many, a slice a
+// block; it is asked for without a device, so it and the grid count on a B200's SMs.
+constexpr int kSms = 148;
 int norm_backward_blocks(const Shape& s) { return std::max(1, (s.nv == 2 ? 18 : 16) / (s.warps * s.teams)); }
 int64_t norm_backward_slices(int64_t rows, int64_t cols) {
     const Shape s = norm_backward_shape(cols);
-    return std::min<int64_t>((rows + s.teams - 1) / s.teams, 148 * norm_backward_blocks(s));
+    return std::min<int64_t>((rows + s.teams - 1) / s.teams, kSms * norm_backward_blocks(s));
 }
 
 template <int DT, bool VEC, bool LEAD>
@@ -873,7 +878,7 @@ auto norm_backward_kernel(int nv) {
 // Where rows start: all (and the weights) on 16 bytes; all matrices' the same way, row by row; anything else.
 enum class Starts { kEven, kShared, kAny };
 // Launches the gradient; how many slices of partial sums it writes, or -1.  Rows of a layer of any width, contiguous in all matrices,
-// are the ordinary case of kShared: 8192 x 4099 takes 61.8 us with their vectors, 84.5 by elements at any place.
+// are the ordinary case of kShared: 8192 x 4099 takes 62 us with their vectors, 84.5 by elements at any place.
 template <int DT>
 int64_t launch_norm_backward(const NormBackArgs& a, Starts starts, cudaStream_t st) {
     static std::atomic<uint64_t> done[3][4];
@@ -887,10 +892,10 @@ int64_t launch_norm_backward(const NormBackArgs& a, Starts starts, cudaStream_t 
     while (blocks > 1 && kRoom / blocks < 2 * stage) --blocks;
     const int stages = (int)std::min<size_t>(3, kRoom / blocks / stage);
     if (s.nv == 0 || stages < 2) {
-        const int64_t grid = std::min<int64_t>(a.rows, 148);
+        const int64_t grid = std::min<int64_t>(a.rows, kSms);
         return launch_chained(starts == Starts::kEven ? k_norm_backward_long<DT, true> : k_norm_backward_long<DT, false>, (unsigned)grid, 512, 0, st, 1, a) ? grid : -1;
     }
-    int64_t grid = std::min<int64_t>((a.rows + s.teams - 1) / s.teams, 148 * blocks);
+    int64_t grid = std::min<int64_t>((a.rows + s.teams - 1) / s.teams, kSms * blocks);
     // a team's rows have one lead: it steps over a multiple of 8 rows
     if (vec && starts == Starts::kShared && grid * s.teams < a.rows) grid -= grid * s.teams % 8 / s.teams;
     const dim3 block(32 * s.warps, s.teams);

@@ -385,6 +385,26 @@ def test_silu_gate_backward_against_differences_and_in_place():
     assert torch.equal(a, dg) and torch.equal(b, du)
 
 
+def test_gates_of_every_size():
+    """The sigmoid's argument is rounded to fp32 before its power of two, and so is that factor's constant: each leaves an error of |gate| units
+    of 2^-24 at most; the power, the reciprocal and the sum between them take twelve more.  Above 17 the sum is 1."""
+    rows, cols = 400, 1001
+    g = gen(6)
+    gate = (torch.rand(rows, cols, generator=g, device="cuda") * 2 - 1) * 87.3
+    dy, up = (torch.randn(rows, cols, generator=g, device="cuda") for _ in range(2))
+    dg, du = torch.empty_like(gate), torch.empty_like(gate)
+    R.silu_gate_q8_backward(dy, gate, up, dg, du)
+    d, a, b = dy.double(), gate.double(), up.double()
+    s = 1 / (1 + torch.exp(-a))
+    least = 2.0 ** -126 * (1 + a.abs()) * (1 + d.abs())                # (what is below fp32's normal numbers)
+    eu = d * a * s
+    assert torch.all((du.double() - eu).abs() <= (2 * a.abs() + 14) * P.U32 * eu.abs() + least)
+    size = (d * b * s).abs() * (1 + (a * (1 - s)).abs())
+    assert torch.all((dg.double() - d * b * s * (1 + a * (1 - s))).abs() <= (3 * a.abs() + 16) * P.U32 * size + least * (1 + b.abs()))
+    out = R.silu_gate_q8(gate, up, R.RowsQ8(rows, cols))
+    P.check_rows(out, P.silu_gate(a, b), eps=(2 * 87.3 + 16) * P.U32)
+
+
 def test_large_gates_saturate():
     gate = torch.tensor([[-200.0, -90.0, -88.0, -50.0, 50.0, 88.0, 90.0, 200.0, 0.0, -0.0]], device="cuda")
     ones = torch.ones_like(gate)
