@@ -131,10 +131,10 @@ Rows* rows_of(PyObject* o) {
     if (Py_TYPE(o) != &RowsType) return refuse("rows", "rows in 8 bits", o), nullptr;
     return reinterpret_cast<Rows*>(o);
 }
-// The first rows x cols of a tensor, unit column stride, within its storage.
+// The first rows x cols of a tensor, unit column stride, within its storage (looked at without counting a reference to it).
 bool holds(const at::Tensor& t, int64_t rows, int64_t cols) {
     if (rows == 0 || cols == 0) return true;
-    return (t.storage_offset() + (rows - 1) * t.stride(0) + cols) * (int64_t)t.itemsize() <= (int64_t)t.storage().nbytes();
+    return (t.storage_offset() + (rows - 1) * t.stride(0) + cols) * (int64_t)t.itemsize() <= (int64_t)t.unsafeGetTensorImpl()->unsafe_storage().nbytes();
 }
 // Whether the originals of rows that were laid out anew are both there and have been written since.
 bool changed(const Rows* r) {
